@@ -65,8 +65,10 @@ enum {
     SPA_ERR_BAD_STRIDE = -4,          /* stride not a multiple of 8 / pointer not 16-B aligned */
     SPA_ERR_WORKSPACE_TOO_SMALL = -5, /* ws_bytes < spa_workspace_bytes()                   */
     SPA_ERR_LAUNCH = -6,              /* the HIP runtime rejected a launch                  */
-    SPA_ERR_STATIC_SCRATCH_TOO_SMALL = -7 /* sparse_prefill_select_static: the call needs more than
+    SPA_ERR_STATIC_SCRATCH_TOO_SMALL = -7, /* sparse_prefill_select_static: the call needs more than
                                          SPA_STATIC_SCRATCH_BYTES of scratch                 */
+    SPA_ERR_OVERLAP = -8              /* sparse_prefill_paged_plan: an array that is written
+                                         overlaps another one                                */
 };
 
 typedef struct spa_params {
@@ -363,6 +365,102 @@ int sparse_prefill_fused_ex(const spa_params *p, const void *q, const void *k, c
                             const spa_select_opts *opts, void *out, float *lse_or_null,
                             int32_t *block_idx_or_null, int32_t *block_cnt_or_null, void *ws,
                             size_t ws_bytes, void *hip_stream);
+
+/* ---- Paged KV cache: what follows the prefill ------------------------------------------------
+ * The prefill of Sec. 4.1 exists to fill a KV cache ("KV Cache Generation stage").  The calls below
+ * keep that cache in pages and attend to it: the tables of one serving step are built on the device,
+ * the step's new keys and values go to their pages, and the new tokens of every request (one each in a
+ * decode step, a few drafted ones, a chunk of a prompt) attend to all that the request has cached.
+ *
+ *   k_pages   [n_pages, n_kv_heads, page_size, head_dim] bf16
+ *   vt_pages  [n_pages, n_kv_heads, head_dim, page_size] bf16: V transposed per page, as in
+ *             sparse_prefill_transpose_v (both matrix-core operands are then plain 16-byte reads)
+ *             The two inner axes are contiguous; the strides of the page and head axes come from
+ *             kp_stride / vp_stride, so K and V may share one allocation.  A slot is a token's place:
+ *             page * page_size + offset in the page.
+ *   block_table [batch, max_pages] int32, rows table_stride apart: page of tokens j * page_size ..  of
+ *             request b.  Entries of pages that hold no key that a query of the call may see are not
+ *             looked at for their value: they may be anything.
+ *   q_starts  [batch + 1] int32: the new tokens of request b are the rows q_starts[b] ..
+ *             q_starts[b + 1] - 1 of q, k, v, out, slots: requests packed one after the other, the rows
+ *             behind the last one are padding (not read, not written).
+ *   kv_lens   [batch] int32: tokens of request b in the cache, the new ones included: its i-th of n new
+ *             tokens has position kv_lens[b] - n + i.
+ * Lengths and tables are read on the device: no call needs them on the host, and a captured graph may
+ * be replayed with others.  A malformed one (a page outside the cache, a length past max_pages, starts
+ * that are not ascending) cannot make a kernel leave the tensors; the rows concerned are unspecified. */
+typedef struct spa_paged_params {
+    int32_t batch;          /* 1 .. 4096 requests                                               */
+    int32_t n_q_heads;      /* >= 1, multiple of n_kv_heads                                     */
+    int32_t n_kv_heads;     /* >= 1                                                             */
+    int32_t head_dim;       /* 64 or 128                                                        */
+    int32_t page_size;      /* 16, 32, 64 or 128 tokens                                         */
+    int32_t n_pages;        /* >= 1 pages in the cache; n_pages * page_size < 2^31              */
+    int32_t max_pages;      /* >= 1 columns of block_table; max_pages * page_size <= 2^30       */
+    int32_t n_tokens;       /* 1 .. 2^24 rows of q, k, v, out, slots; n_tokens * n_q_heads < 2^31 */
+    int32_t max_new_tokens; /* sparse_prefill_paged_attn: the most new tokens a request of the call
+                               has, as far as the host knows (0: not known).  It chooses among
+                               kernels; results do not depend on it being right                 */
+    float softmax_scale;    /* 0 selects 1/sqrt(head_dim)                                       */
+    int32_t n_sink_tokens;  /* >= 0 } with window_tokens = w > 0 the query at position i sees the keys */
+    int32_t window_tokens;  /* >= 0 } j <= i with i - j < w or j < n_sink_tokens (the A-shape of
+                               Sec. 4.1.1, by tokens); with w = 0 every key j <= i              */
+    float softcap;          /* 0: none.  c > 0: a scaled logit s becomes c * tanh(s / c)        */
+    int64_t table_stride;   /* >= max_pages elements                                            */
+    int64_t q_stride[2];    /* elements: token, head; the head_dim axis is contiguous           */
+    int64_t k_stride[2];
+    int64_t v_stride[2];
+    int64_t o_stride[2];    /* both >= head_dim                                                 */
+    int64_t kp_stride[2];   /* elements: page, head; both >= page_size * head_dim               */
+    int64_t vp_stride[2];
+} spa_paged_params;
+
+/* Bytes of device scratch that sparse_prefill_paged_attn needs in `ws`.  Host only. */
+int spa_paged_workspace_bytes(const spa_paged_params *p, size_t *bytes);
+
+/* Block tables and slot maps of one step, from the requests' lengths: request b holds ctx_lens[b] tokens
+ * and brings new_lens[b] more.  It needs the pages ceil(ctx / page_size) .. ceil((ctx + new) / page_size) - 1
+ * in addition to those it has.  In the order of the requests these are taken from
+ * free_pages[free_range[0] .. free_range[1] - 1], first to first, and written into its row of block_table (no
+ * other entry is touched).  A request whose pages the free list cannot cover is left out, with all behind it
+ * that need pages too; so is one with a negative length, with ctx + new > max_pages * page_size, or with tokens
+ * past n_tokens.
+ *   q_starts  [batch + 1]: running sum of new_lens (of requests left out, too), at most n_tokens
+ *   kv_lens   [batch]: ctx + new, or 0 for a request that is left out: it then attends to nothing
+ *   slots     [n_tokens]: place of every new token, -1 for a request left out, for padding, and where the
+ *             table names a page outside the cache
+ *   positions_or_null [n_tokens]: position of every new token in its request, 0 for padding
+ *   taken     [2]: pages taken from the free list, requests left out
+ * free_pages: n_free >= 0 int32 (NULL if there are none); free_range: 2 int32 on the device, clamped to
+ * [0, n_free].  No array that is written may overlap another one.
+ * Uses of p: batch, page_size, n_pages, max_pages, n_tokens, table_stride. */
+int sparse_prefill_paged_plan(const spa_paged_params *p, const int32_t *ctx_lens, const int32_t *new_lens,
+                              const int32_t *free_pages, int32_t n_free, const int32_t *free_range,
+                              int32_t *block_table, int32_t *q_starts, int32_t *kv_lens, int32_t *slots,
+                              int32_t *positions_or_null, int32_t *taken, void *hip_stream);
+
+/* Keys and values of the new tokens into their pages: k, v [n_tokens, n_kv_heads, head_dim] (strides
+ * k_stride, v_stride), token t to slots[t]; a slot outside the cache (-1 for padding) is passed over.  Every
+ * other token of the cache keeps its bits.  A slot that occurs twice ends up with either token's values.
+ * Uses of p: n_kv_heads, head_dim, page_size, n_pages, n_tokens, strides. */
+int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const void *v, const int32_t *slots,
+                                void *k_pages, void *vt_pages, void *hip_stream);
+
+/* Attention of the new tokens over their requests' pages (the new tokens' own keys are in the cache already):
+ * for the query at position i of head h
+ *   x_j = softmax_scale * q . k_j,  capped by softcap,  minus slopes[h] * (i - j),   over the keys j it sees
+ *   out = sum_j softmax(x)_j v_j
+ * in fp32 with bf16 matrix products; out [n_tokens, n_q_heads, head_dim] bf16.  slopes_or_null: n_q_heads fp32
+ * on the device (bias by distance).  lse_or_null: [n_tokens, n_q_heads] fp32, ln sum_j e^x_j.  A query that
+ * sees no key (kv_lens[b] = 0, or a position below 0) gets zeros and -inf.  Values behind the last key that a
+ * query sees never reach it, whatever they are, when it is its request's only one; among the queries of one
+ * request an infinite or NaN value may also reach queries up to 127 tokens away from those that see it.
+ * ws: spa_paged_workspace_bytes() bytes, 256-byte aligned; its contents need not survive between calls, calls
+ * that overlap in time need one each. */
+int sparse_prefill_paged_attn(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,
+                              const int32_t *block_table, const int32_t *q_starts, const int32_t *kv_lens,
+                              const float *slopes_or_null, void *out, float *lse_or_null, void *ws,
+                              size_t ws_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

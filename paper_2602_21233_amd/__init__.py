@@ -6,6 +6,8 @@ kernels.  PyTorch supplies device memory and the current stream.
 """
 from .binding import (SpaError, attn, attn_vt, check_lists, fused, library_path, load_library, pool, row_capacity, select,
                       select_static, topk_from_scores, transpose_v, value_norms, workspace_bytes)
+from .paged import make_paged_params, paged_append, paged_attn, paged_plan, paged_workspace_bytes
 
-__all__ = ["SpaError", "attn", "attn_vt", "check_lists", "fused", "library_path", "load_library", "pool", "row_capacity",
+__all__ = ["SpaError", "attn", "attn_vt", "check_lists", "fused", "library_path", "load_library", "make_paged_params", "paged_append",
+           "paged_attn", "paged_plan", "paged_workspace_bytes", "pool", "row_capacity",
            "select", "select_static", "topk_from_scores", "transpose_v", "value_norms", "workspace_bytes"]

@@ -18,7 +18,8 @@ EXPORTS = ("spa_strerror", "spa_row_capacity", "spa_workspace_bytes", "sparse_pr
            "sparse_prefill_fused_tpd", "sparse_prefill_value_norms", "sparse_prefill_select_stem",
            "sparse_prefill_fused_stem", "sparse_prefill_select_ex", "sparse_prefill_topk_from_scores_ex",
            "sparse_prefill_fused_ex", "sparse_prefill_check_lists", "sparse_prefill_select_static",
-           "sparse_prefill_transpose_v", "sparse_prefill_attn_vt")
+           "sparse_prefill_transpose_v", "sparse_prefill_attn_vt", "spa_paged_workspace_bytes", "sparse_prefill_paged_plan",
+           "sparse_prefill_paged_append", "sparse_prefill_paged_attn")
 
 
 class SpaError(RuntimeError):
@@ -48,6 +49,14 @@ assert _PARAMS.size == ctypes.sizeof(SpaParams)
 class SpaSelectOpts(ctypes.Structure):
     _fields_ = [("top_k_per_block", ctypes.c_void_p), ("v", ctypes.c_void_p), ("head_pattern", ctypes.c_void_p),
                 ("mass_gamma", ctypes.c_float)]
+
+
+class SpaPagedParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages",
+                                              "n_tokens", "max_new_tokens")]
+    _fields_ += [("softmax_scale", ctypes.c_float), ("n_sink_tokens", ctypes.c_int32), ("window_tokens", ctypes.c_int32),
+                 ("softcap", ctypes.c_float), ("table_stride", ctypes.c_int64)]
+    _fields_ += [(n + "_stride", ctypes.c_int64 * 2) for n in ("q", "k", "v", "o", "kp", "vp")]
 
 
 def library_path() -> str:
@@ -86,6 +95,11 @@ def load_library():
     lib.sparse_prefill_select_ex.argtypes = [pp, vp, vp, po, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.sparse_prefill_topk_from_scores_ex.argtypes = [pp, vp, po, vp, vp, vp]
     lib.sparse_prefill_fused_ex.argtypes = [pp, vp, vp, vp, po, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    pg = ctypes.POINTER(SpaPagedParams)
+    lib.spa_paged_workspace_bytes.argtypes = [pg, ctypes.POINTER(ctypes.c_size_t)]
+    lib.sparse_prefill_paged_plan.argtypes = [pg, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sparse_prefill_paged_append.argtypes = [pg, vp, vp, vp, vp, vp, vp]
+    lib.sparse_prefill_paged_attn.argtypes = [pg, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     for name in EXPORTS[1:]:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib

@@ -246,6 +246,7 @@ const char* spa_strerror(int code) {
         case SPA_ERR_WORKSPACE_TOO_SMALL: return "workspace smaller than spa_workspace_bytes()";
         case SPA_ERR_LAUNCH: return "the HIP runtime rejected a kernel launch";
         case SPA_ERR_STATIC_SCRATCH_TOO_SMALL: return "the call needs more scratch than the library's static device array holds (SPA_STATIC_SCRATCH_BYTES); use the call that takes a workspace";
+        case SPA_ERR_OVERLAP: return "an array that the call writes overlaps another of its arrays";
         default: return "unknown error code";
     }
 }

@@ -1,0 +1,517 @@
+// Attention of new tokens over a paged KV cache: single tokens, a few of them, chunks of prompts.
+//
+// The rows of a workgroup are (new token, query head) pairs of one KV head, so that a group's heads take every key and value
+// from one load.  The key axis of a row tile is cut into pieces so that few rows fill the chip, too; pieces leave a normalised
+// partial result and its log-sum-exp, merged by a second kernel.  How a call is cut depends on lengths that only the device
+// knows: every wavefront derives its share from them by itself (share_of_workgroup), without a plan, a host copy or a barrier.
+//
+// Softmax in base 2: x = (scaled logit) * log2 e, weights 2^(x - m) against a reference m that is set by the first tile and
+// moved only when a query's running denominator passes 2^40; the normalisation makes the result independent of m.  Logits,
+// weights' sums and outputs are held in fp32; the weights are rounded to bf16 for the second matrix product, whose other
+// operand is bf16 anyway: an error of at most 2^-9 of each term, below the rounding of the bf16 output on sums of many.
+#include "paged.hpp"
+
+namespace spa {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kRescaleAt = 1.099511627776e12f;      // 2^40
+
+struct PagedArgs {
+    const uint16_t *q, *k, *vt;
+    const int32_t *table, *q_starts, *kv_lens;
+    const float* slopes;                              // nullptr: no bias by distance
+    uint16_t* out;
+    float* lse;                                       // nullptr: not wanted
+    int B, Hq, Hkv, G, T, log_p, n_pages, C, sink, window;
+    float scale, cap;                                 // cap 0: none
+    int64_t table_stride, q_t, q_h, o_t, o_h, kp_p, kp_h, vp_p, vp_h;
+};
+
+// ---------------------------------------------------------------------------------------------------------------
+// How a call is cut
+
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {                             // inclusive, over the lanes
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, true);   // row_shr:1, lanes shifted out read 0
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, true);   // row_shr:2
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, true);   // row_shr:4
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, true);   // row_shr:8
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, true);   // row_bcast15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, true);   // row_bcast31 into rows 2 and 3
+    return v;
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
+
+struct Request {
+    int first, len, kv;               // first row and number of its new tokens, cached tokens
+};
+__device__ __forceinline__ Request request_at(const PagedArgs& a, int b) {
+    Request r{0, 0, 0};
+    if (b < a.B) {
+        r.first = clamp_int(a.q_starts[b], 0, a.T);
+        r.len = clamp_int(a.q_starts[b + 1], r.first, a.T) - r.first;
+        r.kv = clamp_int(a.kv_lens[b], 0, a.C << a.log_p);
+    }
+    return r;
+}
+__device__ __forceinline__ PagedShare share_at(const PagedArgs& a, const PagedPart& part, const Request& r, int piece) {
+    return paged_share(part, a.G, r.len, r.kv, a.sink, a.window, piece);
+}
+// key tiles of a part's pieces, the same in every lane
+__device__ __forceinline__ int part_piece(const PagedArgs& a, const PagedPart& part, int lane) {
+    int64_t work = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const PagedShare s = share_at(a, part, request_at(a, b0 + lane), 1 << 24);
+        work += (int64_t)s.tiles * s.keys;
+    }
+    // the lanes' sum in two halves of 24 bits; a lane's work of 2^48 and more makes the piece as long as any key axis either way
+    const uint32_t lo = last_lane(wave_scan((uint32_t)(work & 0xffffff)));
+    const uint32_t hi = last_lane(wave_scan((uint32_t)(work >> 24 > 0xffffff ? 0xffffff : work >> 24)));
+    return piece_of((((int64_t)hi << 24) + lo) * a.Hkv, part);
+}
+
+// What a workgroup of a part serves: unit `unit` of request b, counted from the longest row tiles, KV heads next to each
+// other (they go to different XCDs, each of which then keeps its heads' keys in its L2).
+struct Share {
+    int b, unit;                      // b < 0: nothing
+    int slot;                         // first partial result of the request (its units' results follow each other)
+    PagedShare s;
+    Request r;
+};
+// MERGE: units are those of the merge kernel, m / 16 for each (row tile, KV head) of a request whose keys are cut
+template <bool MERGE>
+__device__ __forceinline__ Share share_of_workgroup(const PagedArgs& a, const PagedPart& part, uint32_t item) {
+    const int lane = threadIdx.x & 63;
+    const int piece = part_piece(a, part, lane);
+    uint32_t items_before = 0, slots_before = 0;
+    Share found;
+    found.b = -1;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const Request r = request_at(a, b0 + lane);
+        const PagedShare s = share_at(a, part, r, piece);
+        const uint32_t units = (uint32_t)s.tiles * (uint32_t)s.splits * (uint32_t)a.Hkv;
+        const uint32_t slots = s.splits > 1 ? units : 0u;
+        const uint32_t items = !MERGE ? units : (s.splits > 1 ? (uint32_t)s.tiles * (uint32_t)a.Hkv * (uint32_t)(part.m / 16) : 0u);
+        const uint32_t items_upto = items_before + wave_scan(items), slots_upto = slots_before + wave_scan(slots);
+        const uint64_t here = __ballot(item >= items_upto - items && item < items_upto);
+        if (here != 0) {
+            const int at = __builtin_ctzll(here);
+            auto pick = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+            found.b = b0 + at;
+            found.unit = (int)(item - (uint32_t)pick((int)(items_upto - items)));
+            found.slot = pick((int)(slots_upto - slots));
+            found.s = PagedShare{pick(s.tiles), pick(s.keys), pick(s.splits)};
+            found.r = Request{pick(r.first), pick(r.len), pick(r.kv)};
+            return found;
+        }
+        items_before = last_lane(items_upto);
+        slots_before = last_lane(slots_upto);
+    }
+    return found;
+}
+// a request's key tiles are dealt to its pieces evenly
+__device__ __forceinline__ int tiles_of_piece(const PagedShare& s) { return (int)((uint32_t)(s.keys + s.splits - 1) / (uint32_t)s.splits); }
+
+// ---------------------------------------------------------------------------------------------------------------
+// Few rows: MF * 16 rows, four wavefronts that each take every fourth 32 keys, straight from memory into the operands of
+// v_mfma_f32_16x16x32_bf16 (S^T = K Q^T, O^T += V^T P^T).  A lane holds keys 8 (lane / 16) .. + 7 of a chunk of one row:
+// K rows are assigned to the first product's rows such that the weights are the second one's operand as they are.  Bound
+// by HBM: nothing is shared between the wavefronts, so there is no LDS in the loop and no barrier.
+
+// base-2 logits of a lane: what the options make of scaled products
+struct Logits {
+    float c;                          // scale * log2 e
+    float cap, cap_inv2, cap2;        // cap > 0: 2 * scale * log2 e / cap, cap * log2 e
+    float slope2;                     // slope * log2 e
+};
+__device__ __forceinline__ Logits logits_of(const PagedArgs& a, int head) {
+    Logits l;
+    l.c = a.scale * kLog2e;
+    l.cap = a.cap;
+    l.cap_inv2 = a.cap > 0.f ? 2.f * l.c / a.cap : 0.f;
+    l.cap2 = a.cap * kLog2e;
+    l.slope2 = a.slopes != nullptr ? a.slopes[head] * kLog2e : 0.f;
+    return l;
+}
+// back: position of the query less that of the key
+template <bool MOD>
+__device__ __forceinline__ float logit(const Logits& l, float s, int back) {
+    if constexpr (!MOD) {
+        return s * l.c;
+    } else {
+        float x = s * l.c;
+        // tanh |y| = (1 - t) / (1 + t), t = e^(-2 |y|) <= 1: nothing overflows, absolute error about 2^-25 near 0
+        if (l.cap > 0.f) {
+            const float t = __builtin_amdgcn_exp2f(-fabsf(s * l.cap_inv2));
+            x = __builtin_copysignf(l.cap2 * (1.f - t) * __builtin_amdgcn_rcpf(1.f + t), s);
+        }
+        return fmaf(-l.slope2, (float)back, x);
+    }
+}
+
+__device__ __forceinline__ float max_over_groups(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
+__device__ __forceinline__ float sum_over_groups(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
+
+template <int D, int MF, bool MOD, bool SMALL>
+__global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs a, PagedPart part) {
+    constexpr int NW = 4;
+    constexpr int DS = D / 32;        // MFMAs of a logits tile
+    constexpr int DT = D / 16;        // 16-row tiles of O^T
+    constexpr int PAD = D + 4;
+    __shared__ __attribute__((aligned(16))) float s_o[NW][16][PAD];
+    __shared__ float s_m[NW][MF * 16], s_l[NW][MF * 16];
+
+    const Share sh = share_of_workgroup<false>(a, part, blockIdx.x);
+    if (sh.b < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n16 = lane & 15, g = lane >> 4;
+    const int kvh = sh.unit % a.Hkv, cut = sh.unit / a.Hkv % sh.s.splits, tile = sh.s.tiles - 1 - sh.unit / a.Hkv / sh.s.splits;
+    const int rows = sh.r.len * a.G, row0 = tile * part.m;
+    const int last_row = min(row0 + part.m, rows) - 1;
+    const int pos0 = sh.r.kv - sh.r.len;                        // position of the request's first new token
+    const int pos_lo = pos0 + row0 / a.G, pos_hi = pos0 + last_row / a.G;
+    const KeyTiles kt = key_tiles(pos_lo, pos_hi, a.sink, a.window);
+    const int per = tiles_of_piece(sh.s);
+    const int e_end = min((cut + 1) * per, kt.n);               // of the row tile's key tiles
+    const int last_col = pos_hi >= 0 ? pos_hi >> a.log_p : 0;
+    const int page = 1 << a.log_p;
+
+    bf16x8 qf[MF][DS];
+    int pos[MF], head[MF], token[MF];
+    Logits lg[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+        const int row = min(row0 + 16 * f + n16, last_row);      // rows past the last repeat it; they are not stored
+        token[f] = row / a.G;
+        head[f] = kvh * a.G + row % a.G;
+        pos[f] = pos0 + token[f];
+        const uint16_t* qrow = a.q + (int64_t)(sh.r.first + token[f]) * a.q_t + head[f] * a.q_h + 8 * g;
+#pragma unroll
+        for (int s = 0; s < DS; ++s) qf[f][s] = *reinterpret_cast<const bf16x8*>(qrow + 32 * s);
+        lg[f] = logits_of(a, head[f]);
+    }
+    f32x4 o[MF][DT];
+    float m[MF], l[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+        m[f] = -INFINITY;
+        l[f] = 0.f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int32_t* const trow = a.table + (int64_t)sh.b * a.table_stride;
+    auto page_of = [&](int key) { return clamp_int(trow[min(key >> a.log_p, last_col)], 0, a.n_pages - 1); };
+    const int k_row = 8 * (n16 >> 2) + (n16 & 3);               // key of a chunk that this lane loads, and + 4
+
+    for (int c = 2 * cut * per + wave; c < 2 * e_end; c += NW) {
+        const int key0 = kt.at(c >> 1) * kPagedTile + 32 * (c & 1);
+        if (key0 > pos_hi) break;                               // only the last tile's second half
+        int id_k = page_of(key0), id_v = id_k;
+        if constexpr (SMALL) {                                  // pages of 16 tokens: a chunk lies in two
+            const int id1 = page_of(key0 + 16);
+            if (n16 >= 8) id_k = id1;
+            if (g >= 2) id_v = id1;
+        }
+        const int in_page = SMALL ? 0 : key0 & (page - 1);
+        const uint16_t* kp = a.k + id_k * a.kp_p + kvh * a.kp_h + (in_page + (SMALL ? k_row & 15 : k_row)) * D + 8 * g;
+        const uint16_t* vp = a.vt + id_v * a.vp_p + kvh * a.vp_h + in_page + 8 * (SMALL ? g & 1 : g) + (int64_t)n16 * page;
+        bf16x8 k0[DS], k1[DS];
+        u32x4 vv[DT];
+#pragma unroll
+        for (int s = 0; s < DS; ++s) {
+            k0[s] = *reinterpret_cast<const bf16x8*>(kp + 32 * s);
+            k1[s] = *reinterpret_cast<const bf16x8*>(kp + 4 * D + 32 * s);
+        }
+#pragma unroll
+        for (int t = 0; t < DT; ++t) vv[t] = *reinterpret_cast<const u32x4*>(vp + 16 * t * page);
+
+        // keys that no row of the tile sees: behind its last position, or between the sinks and its first window
+        const int gone_lo = a.sink, gone_hi = a.window > 0 ? pos_lo - a.window + 1 : 0;       // [gone_lo, gone_hi)
+        if (key0 + 31 > pos_hi || (key0 + 31 >= gone_lo && key0 < gone_hi)) {
+            const int key = key0 + 8 * g;
+            u32x4 keep;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int ka = key + 2 * x, kb = ka + 1;
+                keep[x] = (ka <= pos_hi && !(ka >= gone_lo && ka < gone_hi) ? 0xffffu : 0u) |
+                          (kb <= pos_hi && !(kb >= gone_lo && kb < gone_hi) ? 0xffff0000u : 0u);
+            }
+#pragma unroll
+            for (int t = 0; t < DT; ++t) vv[t] &= keep;
+        }
+        const bool masked = key0 + 31 > pos_lo || (a.window > 0 && key0 + 31 >= a.sink && key0 <= pos_hi - a.window);
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+            f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+            for (int s = 0; s < DS; ++s) {
+                s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0[s], qf[f][s], s0, 0, 0, 0);
+                s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1[s], qf[f][s], s1, 0, 0, 0);
+            }
+            f32x8 x;
+            const int back = pos[f] - key0 - 8 * g;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[r] = logit<MOD>(lg[f], s0[r], back - r);
+                x[4 + r] = logit<MOD>(lg[f], s1[r], back - 4 - r);
+            }
+            if (masked) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const int b = back - r;
+                    if (b < 0 || (a.window > 0 && b >= a.window && pos[f] - b >= a.sink)) x[r] = -INFINITY;
+                }
+            }
+            const float mr = m[f] == -INFINITY ? 0.f : m[f];
+            f32x8 w;
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                w[r] = __builtin_amdgcn_exp2f(x[r] - mr);
+                sum += w[r];
+            }
+            if (__any(m[f] == -INFINITY || !(l[f] + sum < kRescaleAt))) {
+                float mx = x[0];
+#pragma unroll
+                for (int r = 1; r < 8; ++r) mx = fmaxf(mx, x[r]);
+                mx = max_over_groups(mx);
+                const float lq = sum_over_groups(l[f]);
+                const float m_new = fmaxf(m[f] == -INFINITY ? m[f] : m[f] + (lq > 1.f ? __log2f(lq) : 0.f), mx);
+                const float alpha = m[f] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[f] - m_new);
+                m[f] = m_new;
+                l[f] *= alpha;
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[f][t][r] *= alpha;
+                const float mn = m_new == -INFINITY ? 0.f : m_new;
+                sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    w[r] = __builtin_amdgcn_exp2f(x[r] - mn);
+                    sum += w[r];
+                }
+            }
+            l[f] += sum;
+            const bf16x8 p = __builtin_convertvector(w, bf16x8);
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+                o[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vv[t]), p, o[f][t], 0, 0, 0);
+        }
+    }
+
+    // The four wavefronts' results of a row become one: every wavefront leaves its sums, relative to its own reference
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+        const float lq = sum_over_groups(l[f]);
+        if (g == 0) { s_m[wave][16 * f + n16] = m[f]; s_l[wave][16 * f + n16] = lq; }
+    }
+    const bool partial = sh.s.splits > 1;
+    const int slot = sh.slot + sh.unit;
+    if (partial && slot >= part.n_slots) return;                // starts that are not ascending: more units than there is room for
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+        if (f > 0) __syncthreads();
+#pragma unroll
+        for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(&s_o[wave][n16][16 * t + 4 * g]) = o[f][t];
+        __syncthreads();
+        const int r16 = tid >> 4, d0 = (tid & 15) * (D / 16);    // 16 threads a row, D / 16 values each
+        const int row = row0 + 16 * f + r16;
+        if (row <= last_row) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) mx = fmaxf(mx, s_m[w][16 * f + r16]);
+            float lsum = 0.f, acc[D / 16];
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) acc[x] = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float mw = s_m[w][16 * f + r16];
+                const float scale = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - mx);
+                lsum = fmaf(s_l[w][16 * f + r16], scale, lsum);
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) acc[x] = fmaf(s_o[w][r16][d0 + x], scale, acc[x]);
+            }
+            const bool none = mx == -INFINITY && lsum == 0.f;    // a row that sees no key (of this piece); NaN is not none
+            const float inv = none ? 0.f : 1.f / lsum;
+            const float lse2 = none ? -INFINITY : mx + __log2f(lsum);
+            if (partial) {
+                float* po = part.o + ((int64_t)slot * part.m + 16 * f + r16) * D + d0;
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) po[x] = acc[x] * inv;
+                if ((tid & 15) == 0) part.lse[(int64_t)slot * part.m + 16 * f + r16] = lse2;
+            } else {
+                const int tok = sh.r.first + row / a.G, hd = kvh * a.G + row % a.G;
+                uint16_t* orow = a.out + (int64_t)tok * a.o_t + hd * a.o_h + d0;
+#pragma unroll
+                for (int x = 0; x < D / 16; x += 4) {
+                    const f32x4 v = {acc[x] * inv, acc[x + 1] * inv, acc[x + 2] * inv, acc[x + 3] * inv};
+                    *reinterpret_cast<bf16x4*>(orow + x) = __builtin_convertvector(v, bf16x4);
+                }
+                if (a.lse != nullptr && (tid & 15) == 0) a.lse[(int64_t)tok * a.Hq + hd] = lse2 * kLn2;
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Merge of the pieces' results: one workgroup for 16 rows, a wavefront per row, D / 8 lanes a piece.
+template <int D>
+__device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& part, uint32_t item) {
+    constexpr int LPR = D / 8, NG = 64 / LPR;       // lanes of a piece, pieces at a time
+    const Share sh = share_of_workgroup<true>(a, part, item);
+    if (sh.b < 0) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int subs = part.m / 16;
+    const int sub = sh.unit % subs, u = sh.unit / subs;
+    const int kvh = u % a.Hkv, rank = u / a.Hkv;    // rank: row tiles from the last one on
+    const int rows = sh.r.len * a.G;
+    const int splits = sh.s.splits;
+    const int slot0 = sh.slot + rank * splits * a.Hkv + kvh;
+    if (slot0 + (splits - 1) * a.Hkv >= part.n_slots) return;
+    for (int r = wave; r < 16; r += 4) {
+        const int rt = 16 * sub + r, row = (sh.s.tiles - 1 - rank) * part.m + rt;
+        if (row >= rows) continue;
+        const float* lse = part.lse + rt;
+        float mx = -INFINITY;
+        bool bad = false;                           // NaN somewhere: fmaxf drops it
+        for (int s = lane; s < splits; s += 64) {
+            const float v = lse[(int64_t)(slot0 + s * a.Hkv) * part.m];
+            bad |= v != v;
+            mx = fmaxf(mx, v);
+        }
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
+        const int d0 = 8 * (lane % LPR);
+        float acc[8], total = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) acc[x] = 0.f;
+        if (mx != -INFINITY || __any(bad)) {
+            for (int s = lane / LPR; s < splits; s += NG) {
+                const int64_t at = (int64_t)(slot0 + s * a.Hkv) * part.m;
+                const float v = lse[at];
+                if (v == -INFINITY) continue;       // an empty piece; its sums may not have been written
+                const float w = __builtin_amdgcn_exp2f(v - mx);
+                const f32x4* po = reinterpret_cast<const f32x4*>(part.o + (at + rt) * D + d0);
+                const f32x4 p0 = po[0], p1 = po[1];
+                total += w;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    acc[x] = fmaf(p0[x], w, acc[x]);
+                    acc[4 + x] = fmaf(p1[x], w, acc[4 + x]);
+                }
+            }
+#pragma unroll
+            for (int x = LPR; x < 64; x <<= 1) {
+                total += __shfl_xor(total, x);
+#pragma unroll
+                for (int y = 0; y < 8; ++y) acc[y] += __shfl_xor(acc[y], x);
+            }
+        }
+        const bool none = total == 0.f;
+        const float inv = none ? 0.f : 1.f / total;
+        if (lane < LPR) {
+            const int tok = sh.r.first + row / a.G, hd = kvh * a.G + row % a.G;
+            f32x8 v;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) v[x] = acc[x] * inv;
+            *reinterpret_cast<bf16x8*>(a.out + (int64_t)tok * a.o_t + hd * a.o_h + d0) = __builtin_convertvector(v, bf16x8);
+            if (a.lse != nullptr && lane == 0) a.lse[(int64_t)tok * a.Hq + hd] = none ? -INFINITY : (mx + __log2f(total)) * kLn2;
+        }
+    }
+}
+template <int D>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a, PagedPart few, PagedPart many, unsigned few_grid) {
+    if (blockIdx.x < few_grid) merge_rows<D>(a, few, blockIdx.x);
+    else merge_rows<D>(a, many, blockIdx.x - few_grid);
+}
+
+// Most workgroups of a part that a call can need, whatever its lengths (below `target` more than without cuts, and none
+// cut into pieces of less than min_tiles)
+int64_t most_units(const PagedDims& d, const PagedPart& part) {
+    const int64_t tiles = ((int64_t)d.T * d.G / part.m + (d.B < d.T ? d.B : d.T)) * d.Hkv;
+    const int64_t keys = (((int64_t)d.C << d.log_p) + kPagedTile - 1) / kPagedTile;
+    const int64_t cuts = (keys + part.min_tiles - 1) / part.min_tiles;
+    const int64_t target = 1ll << part.log_target;
+    return cuts <= 1 || tiles * cuts < tiles + target ? tiles * (cuts > 1 ? cuts : 1) : tiles + target;
+}
+// Most partial results: requests that are cut have at most twice as many pieces as their work fills
+int64_t most_slots(const PagedDims& d, const PagedPart& part) {
+    const int64_t keys = (((int64_t)d.C << d.log_p) + kPagedTile - 1) / kPagedTile;
+    if (keys <= part.min_tiles) return 0;
+    const int64_t units = most_units(d, part), most = 2ll << part.log_target;
+    return units < most ? units : most;
+}
+
+template <int D, int MF>
+void launch_few(const PagedArgs& a, const PagedPart& part, unsigned grid, hipStream_t st) {
+    const bool mod = a.cap > 0.f || a.slopes != nullptr;
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, a, part); };
+    if (a.log_p == 4) {
+        if (mod) go(paged_few_kernel<D, MF, true, true>);
+        else go(paged_few_kernel<D, MF, false, true>);
+    } else {
+        if (mod) go(paged_few_kernel<D, MF, true, false>);
+        else go(paged_few_kernel<D, MF, false, false>);
+    }
+}
+
+template <int D>
+hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts& parts, hipStream_t st) {
+    int64_t few_merges = 0, many_merges = 0;
+    if (parts.few.m) {
+        const int64_t grid = most_units(d, parts.few);
+        if (grid > 0x7fffffffll) return hipErrorInvalidValue;
+        if (parts.few.m == 16) launch_few<D, 1>(a, parts.few, (unsigned)grid, st);
+        else launch_few<D, 2>(a, parts.few, (unsigned)grid, st);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        few_merges = parts.few.n_slots / 2 * (parts.few.m / 16);        // a row tile that is cut has two pieces at least
+    }
+    if (few_merges + many_merges == 0) return hipSuccess;
+    hipLaunchKernelGGL((paged_merge_kernel<D>), dim3((unsigned)(few_merges + many_merges)), dim3(256), 0, st, a, parts.few, parts.many,
+                       (unsigned)few_merges);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+PagedParts paged_parts(const PagedDims& d, void* ws_or_null) {
+    PagedParts p{};
+    p.few.m = d.G <= 16 && (d.max_new == 0 || (int64_t)d.max_new * d.G <= 16 || d.B > 1) ? 16 : 32;
+    p.few.log_m = p.few.m == 16 ? 4 : 5;
+    p.few.span = (p.few.m + d.G - 1) / d.G + 1;
+    p.few.log_target = 11;
+    p.few.min_tiles = 4;
+    p.few.row_lo = 0;
+    p.few.row_hi = 0x7fffffff;
+    size_t off = 0;
+    for (PagedPart* part : {&p.few, &p.many}) {
+        if (part->m == 0) continue;
+        part->n_slots = (int)most_slots(d, *part);
+        char* base = (char*)ws_or_null;
+        part->o = (float*)(base + off);
+        off += (size_t)part->n_slots * part->m * d.D * sizeof(float);
+        part->lse = (float*)(base + off);
+        off += ((size_t)part->n_slots * part->m * sizeof(float) + 255) / 256 * 256;
+    }
+    p.ws_bytes = off;
+    return p;
+}
+
+hipError_t launch_paged_attn(const PagedDims& d, const PagedParts& parts, const void* q, const void* k_pages, const void* vt_pages,
+                             const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens, const float* slopes_or_null,
+                             void* out, float* lse_or_null, hipStream_t st) {
+    const PagedArgs a{(const uint16_t*)q, (const uint16_t*)k_pages, (const uint16_t*)vt_pages, block_table, q_starts, kv_lens, slopes_or_null,
+                      (uint16_t*)out, lse_or_null, d.B, d.Hq, d.Hkv, d.G, d.T, d.log_p, d.n_pages, d.C, d.sink, d.window, d.scale, d.cap,
+                      d.table_stride, d.q_t, d.q_h, d.o_t, d.o_h, d.kp_p, d.kp_h, d.vp_p, d.vp_h};
+    return d.D == 128 ? launch_parts<128>(a, d, parts, st) : launch_parts<64>(a, d, parts, st);
+}
+
+}  // namespace spa
