@@ -9,16 +9,11 @@
 // moved only when a query's running denominator passes 2^40; the normalisation makes the result independent of m.  Logits,
 // weights' sums and outputs are held in fp32; the weights are rounded to bf16 for the second matrix product, whose other
 // operand is bf16 anyway: an error of at most 2^-9 of each term, below the rounding of the bf16 output on sums of many.
+#include "attn_parts.hpp"
 #include "paged.hpp"
 
 namespace spa {
 namespace {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(8))) float f32x8;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kRescaleAt = 1.099511627776e12f;      // 2^40
@@ -361,6 +356,377 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs a, PagedPar
 }
 
 // ---------------------------------------------------------------------------------------------------------------
+// Many rows: 128 of them, 32 to a wavefront, S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_32x32x16_bf16 on key tiles that all
+// four share through LDS: the pipeline step of the sparse prefill's attention kernel (attn.hip: direct loads into a double
+// buffer, logits two 32-key chunks ahead of the second product, one barrier a tile), with pages in place of blocks, masks
+// where a tile needs them instead of in the last block, and logits that may be capped or biased.
+constexpr int kManyRows = 128;
+
+// 16 bytes per lane straight into LDS, each lane from an address of its own
+template <int IMM>
+__device__ __forceinline__ void lds_dma16_from(uint32_t lds_addr, const void* lane_addr) {
+    asm volatile("s_add_u32 m0, %0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :
+                 : "s"(lds_addr), "v"(lane_addr), "i"(IMM)
+                 : "memory", "m0", "scc");
+}
+// this wavefront's direct loads have landed
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+template <int D, bool MOD, bool SMALL>
+__global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPart part) {
+    constexpr int NW = 4;
+    constexpr int KT = kPagedTile;
+    constexpr int DS = D / 16;          // MFMAs of one logits tile
+    constexpr int DT = D / 32;          // 32-row tiles of O^T
+    constexpr int NG = 2 * DS;          // instruction groups of a step
+    constexpr int TILE = KT * D;
+    constexpr int CPR = D / 8;          // 16-byte chunks of a K row
+    constexpr int RPI = 64 / CPR;       // K rows filled by one 1-KB load instruction
+    constexpr int LPW = TILE / 512 / NW;  // 1-KB load instructions per wave per operand per tile
+    constexpr int TILE_B = TILE * 2;
+    constexpr int CHUNK_B = 32 * D * 2;
+    constexpr int DTILE_B = 32 * KT * 2;
+    static_assert(RPI * LPW == 16, "a wavefront loads 16 keys' rows, which lie in one page");
+    __shared__ __attribute__((aligned(1024))) uint16_t smemK[2][TILE];
+    __shared__ __attribute__((aligned(1024))) uint16_t smemV[2][TILE];
+
+    const Share sh = share_of_workgroup<false>(a, part, blockIdx.x);
+    if (sh.b < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int half = lane >> 5, l32 = lane & 31;
+    const int kvh = sh.unit % a.Hkv, cut = sh.unit / a.Hkv % sh.s.splits, tile = sh.s.tiles - 1 - sh.unit / a.Hkv / sh.s.splits;
+    const int rows = sh.r.len * a.G, row0 = tile * kManyRows;
+    const int last_row = min(row0 + kManyRows, rows) - 1;
+    const int pos0 = sh.r.kv - sh.r.len;
+    const int pos_lo = pos0 + row0 / a.G, pos_hi = pos0 + last_row / a.G;      // of the workgroup's rows
+    const KeyTiles kt = key_tiles(pos_lo, pos_hi, a.sink, a.window);
+    const int per = tiles_of_piece(sh.s);
+    const int e0 = cut * per;
+    const int n_st = min((cut + 1) * per, kt.n) - e0;                         // key tiles of this workgroup
+    const bool partial = sh.s.splits > 1;
+    const int slot = sh.slot + sh.unit;
+    if (partial && slot >= part.n_slots) return;
+
+    const int row = min(row0 + 32 * wave + l32, last_row);                    // rows past the last repeat it; they are not stored
+    const bool valid = row0 + 32 * wave + l32 <= last_row;
+    const int token = row / a.G, head = kvh * a.G + row % a.G, pos = pos0 + token;
+    uint16_t* const orow = a.out + (int64_t)(sh.r.first + token) * a.o_t + head * a.o_h;
+    float* const po = part.o + ((int64_t)slot * kManyRows + 32 * wave + l32) * D;
+    float* const plse = part.lse + (int64_t)slot * kManyRows + 32 * wave + l32;
+    if (n_st <= 0) {                                                          // no key in sight (of this piece)
+        if (valid && half == 0) {
+            if (partial) {
+                *plse = -INFINITY;
+            } else {
+#pragma unroll
+                for (int x = 0; x < D / 8; ++x) *reinterpret_cast<u32x4*>(orow + 8 * x) = u32x4{0u, 0u, 0u, 0u};
+                if (a.lse != nullptr) a.lse[(int64_t)(sh.r.first + token) * a.Hq + head] = -INFINITY;
+            }
+        }
+        return;
+    }
+
+    const int last_col = pos_hi >> a.log_p;
+    const int page = 1 << a.log_p;
+    const int32_t* const trow = a.table + (int64_t)sh.b * a.table_stride;
+    const char* const kbase = reinterpret_cast<const char*>(a.k + kvh * a.kp_h);
+    const char* const vbase0 = reinterpret_cast<const char*>(a.vt + kvh * a.vp_h);
+    auto key_of = [&](int t) { return kt.at(e0 + t) * KT; };                  // first key of tile t
+    auto page_of = [&](int key) { return clamp_int(trow[min(key >> a.log_p, last_col)], 0, a.n_pages - 1); };
+    struct Pages {                                                            // of a tile's 16-key pieces (one page without SMALL)
+        int id[SMALL ? 4 : 1];
+    };
+    auto pages_of = [&](int t) {
+        Pages p;
+        const int key0 = key_of(min(t, n_st - 1));
+#pragma unroll
+        for (int x = 0; x < (SMALL ? 4 : 1); ++x) p.id[x] = page_of(key0 + 16 * x);
+        return p;
+    };
+
+    uint32_t k_offb[LPW], v_offb[LPW];
+    int v_chunk[2];                                                           // 8-key chunk of the tile, for even and odd instructions
+#pragma unroll
+    for (int x = 0; x < LPW; ++x) {
+        const int inst = wave * LPW + x;
+        const int krow = RPI * inst + lane / CPR, vrow = 8 * inst + (lane >> 3);
+        k_offb[x] = 2u * (uint32_t)((RPI * x + lane / CPR) * D + (((lane % CPR) ^ swz_k<D>(krow)) << 3));
+        const int chunk = (lane & 7) ^ swz_v(vrow);
+        if (x < 2) v_chunk[x] = chunk;
+        v_offb[x] = 2u * (uint32_t)(vrow * page + (SMALL ? (chunk & 1) : chunk) * 8);
+    }
+    const uint32_t k_dst = lds_address(&smemK[0][0]) + wave * LPW * 1024;
+    const uint32_t v_dst = lds_address(&smemV[0][0]) + wave * LPW * 1024;
+    auto issue_k = [&](auto buf_tag, int t, const Pages& pg) {
+        constexpr int BUF = decltype(buf_tag)::value;
+        const int key = key_of(t) + 16 * wave;                                // this wavefront's 16 keys
+        int id = pg.id[0];
+        if constexpr (SMALL) id = __builtin_amdgcn_readfirstlane(wave == 0 ? pg.id[0] : wave == 1 ? pg.id[1] : wave == 2 ? pg.id[2] : pg.id[3]);
+        const char* const src = kbase + 2 * ((int64_t)id * a.kp_p + (key & (page - 1)) * D);
+        static_for<LPW>([&](auto x_tag) {
+            constexpr int X = decltype(x_tag)::value;
+            lds_dma16<BUF * TILE_B + X * 1024>(k_dst, k_offb[X], src);
+        });
+    };
+    auto issue_v = [&](auto buf_tag, int t, const Pages& pg) {
+        constexpr int BUF = decltype(buf_tag)::value;
+        const int key0 = key_of(t);
+        if constexpr (!SMALL) {
+            const char* const src = vbase0 + 2 * ((int64_t)pg.id[0] * a.vp_p + (key0 & (page - 1)));
+            static_for<LPW>([&](auto x_tag) {
+                constexpr int X = decltype(x_tag)::value;
+                lds_dma16<BUF * TILE_B + X * 1024>(v_dst, v_offb[X], src);
+            });
+        } else {
+            const char* src[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int piece = v_chunk[x] >> 1;
+                const int id = piece == 0 ? pg.id[0] : piece == 1 ? pg.id[1] : piece == 2 ? pg.id[2] : pg.id[3];
+                src[x] = vbase0 + 2 * ((int64_t)id * a.vp_p + ((key0 + 16 * piece) & (page - 1)));
+            }
+            static_for<LPW>([&](auto x_tag) {
+                constexpr int X = decltype(x_tag)::value;
+                lds_dma16_from<BUF * TILE_B + X * 1024>(v_dst, src[X % 2] + v_offb[X]);
+            });
+        }
+    };
+    // Values of keys that no row of the workgroup sees may be anything, NaN too, and a weight of 0 would not hide them: they
+    // become 0 in LDS.  A wavefront does so for what it has loaded itself, before the barrier that publishes the tile.
+    const int gone_hi = a.window > 0 ? pos_lo - a.window + 1 : 0;             // keys sink .. gone_hi - 1 are out of sight
+    auto clear_unseen = [&](auto buf_tag, int t) {
+        constexpr int BUF = decltype(buf_tag)::value;
+        const int key0 = key_of(t);
+        if (key0 + KT - 1 <= pos_hi && !(key0 + KT - 1 >= a.sink && key0 < gone_hi)) return;
+#pragma unroll
+        for (int x = 0; x < LPW; ++x) {
+            u32x4* const at = reinterpret_cast<u32x4*>(reinterpret_cast<char*>(&smemV[BUF][0]) + (wave * LPW + x) * 1024 + lane * 16);
+            u32x4 v = *at;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int ka = key0 + 8 * v_chunk[x % 2] + 2 * y, kb = ka + 1;
+                v[y] &= (ka <= pos_hi && !(ka >= a.sink && ka < gone_hi) ? 0xffffu : 0u) |
+                        (kb <= pos_hi && !(kb >= a.sink && kb < gone_hi) ? 0xffff0000u : 0u);
+            }
+            *at = v;
+        }
+    };
+
+    Pages pg1 = pages_of(1);
+    {
+        const Pages pg0 = pages_of(0);
+        issue_k(IC<0>{}, 0, pg0);
+        issue_v(IC<0>{}, 0, pg0);
+        if (n_st > 1) issue_k(IC<1>{}, 1, pg1);
+    }
+
+    bf16x8 qf[DS];
+    {
+        const uint16_t* const qrow = a.q + (int64_t)(sh.r.first + token) * a.q_t + head * a.q_h + 8 * half;
+#pragma unroll
+        for (int s = 0; s < DS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qrow + 16 * s);
+    }
+    const Logits lg = logits_of(a, head);
+    int kofs[DS], vofs[4];
+    {
+        const int krow = swap_bits23(l32);
+#pragma unroll
+        for (int s = 0; s < DS; ++s) kofs[s] = 2 * (krow * D + (((2 * s + half) ^ swz_k<D>(krow)) << 3));
+#pragma unroll
+        for (int x = 0; x < 4; ++x) vofs[x] = 2 * (l32 * KT + (((2 * x + half) ^ swz_v(l32)) << 3));
+    }
+    const char* const ldsK = reinterpret_cast<const char*>(&smemK[0][0]);
+    const char* const ldsV = reinterpret_cast<const char*>(&smemV[0][0]);
+    auto lds16 = [](const char* p) { return *reinterpret_cast<const bf16x8*>(p); };
+
+    // Running softmax: weights 2^(x c - mc) of logits x, which are products as they come (c = scale * log2 e) or, with MOD, already
+    // in base 2 (c = 1).  m: the reference; -inf until the row has seen a key, and then limit = -1 sends it to the slow path.
+    f32x16 oacc[DT];
+#pragma unroll
+    for (int dc = 0; dc < DT; ++dc)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[dc][r] = 0.f;
+    const float c = MOD ? 1.f : lg.c;
+    float m = -INFINITY, mc = 0.f, l = 0.f, limit = -1.f;
+    auto weights = [&](const f32x16& s, bf16x8& p0, bf16x8& p1) {
+        f32x8 w0, w1;
+        float sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            w0[x] = __builtin_amdgcn_exp2f(fmaf(s[x], c, -mc));
+            w1[x] = __builtin_amdgcn_exp2f(fmaf(s[8 + x], c, -mc));
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) sum += w0[x];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) sum += w1[x];
+        p0 = __builtin_convertvector(w0, bf16x8);
+        p1 = __builtin_convertvector(w1, bf16x8);
+        return sum;
+    };
+    // moves the reference so that the chunk's weights are at most 1 and the denominator so far is about 1 or less
+    auto raise = [&](const f32x16& s, bf16x8& p0, bf16x8& p1) {
+        float mx = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        mx = fmaxf(mx, other_half(mx));
+        const float lq = l + other_half(l);
+        const bool first = m == -INFINITY;
+        const float m_new = fmaxf(first ? m : m + (lq > 1.f ? __log2f(lq) / c : 0.f), mx);
+        const float alpha = first ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * c);
+        m = m_new;
+        mc = m == -INFINITY ? 0.f : m * c;
+        limit = m == -INFINITY ? -1.f : kRescaleAt;
+        l *= alpha;
+#pragma unroll
+        for (int dc = 0; dc < DT; ++dc)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) oacc[dc][r] *= alpha;
+        l += weights(s, p0, p1);
+    };
+
+    const int wave_row = row0 + 32 * wave;                                    // wave-uniform bounds of this wavefront's rows
+    const int wave_lo = pos0 + min(wave_row, last_row) / a.G, wave_hi = pos0 + min(wave_row + 31, last_row) / a.G;
+    // what options and masks make of a chunk's products; register r holds key key0 + 16 (r / 8) + 8 half + r % 8
+    auto finish = [&](f32x16& s, int key0) {
+        const int back = pos - key0 - 8 * half;
+        if constexpr (MOD) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = logit<true>(lg, s[r], back - 16 * (r >> 3) - (r & 7));
+        }
+        if (key0 + 31 > wave_lo || (a.window > 0 && key0 + 31 >= a.sink && key0 <= wave_hi - a.window)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int b = back - 16 * (r >> 3) - (r & 7);
+                if (b < 0 || (a.window > 0 && b >= a.window && pos - b >= a.sink)) s[r] = -INFINITY;
+            }
+        }
+    };
+    // last chunk with a key in sight of this wavefront; the steps behind it only load.  -1: it has no rows
+    int last_chunk = -1;
+    if (wave_row <= last_row && wave_hi >= 0) {
+        const int at = wave_hi / KT;
+        int e = at >= kt.from ? kt.sinks + at - kt.from : min(at, kt.sinks - 1);
+        const bool inside = kt.at(e) == at;
+        last_chunk = e - e0 >= n_st ? 2 * n_st - 1 : 2 * (e - e0) + (inside && (wave_hi & (KT - 1)) < 32 ? 0 : 1);
+    }
+
+    auto step = [&](auto kb_tag, auto vb_tag, auto kc_tag, const f32x16& s_cur, f32x16& s_nxt, const bf16x8& pc0, const bf16x8& pc1, bf16x8& pn0,
+                    bf16x8& pn1, bf16x8 (&f)[4]) {
+        constexpr int KB = decltype(kb_tag)::value, VB = decltype(vb_tag)::value, KC = decltype(kc_tag)::value;
+        const char* const vbase = ldsV + VB * TILE_B;
+        auto operand = [&](auto j_tag) {            // operand j of this step (j < NG) or of the next one
+            constexpr int J = decltype(j_tag)::value;
+            constexpr int j = J % NG;
+            constexpr int kc = KC + J / NG;
+            const char* const kb2 = ldsK + KB * TILE_B + kc * CHUNK_B;
+            if constexpr (j % 2 == 0) return lds16(kb2 + kofs[j / 2]);
+            else return lds16(vbase + vofs[2 * kc + (j / 2) / DT] + ((j / 2) % DT) * DTILE_B);
+        };
+        f32x8 e;
+        float l_new = l;
+        auto group = [&](auto g_tag) {
+            constexpr int g = decltype(g_tag)::value;
+            group_mfma<g, D>(f[g % 4], qf, s_nxt, oacc, pc0, pc1);
+            if constexpr (g + 3 < NG || KC == 0) f[(g + 3) % 4] = operand(IC<g + 3>{});
+            group_weights<g, D, true>(s_cur, c, mc, e, pn0, pn1, l_new);
+            SPA_FENCE();
+        };
+        SPA_FENCE();
+        static_for<NG>([&](auto g_tag) { group(g_tag); });
+        if (__any(!(l_new < limit))) raise(s_cur, pn0, pn1);
+        else l = l_new;
+    };
+
+    // ---- logits of the two chunks of tile 0, weights of chunk 0
+    wait_for_loads();
+    clear_unseen(IC<0>{}, 0);
+    __syncthreads();
+    f32x16 sA, sB;                                 // logits of even / odd chunks
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { sA[r] = 0.f; sB[r] = 0.f; }
+#pragma unroll
+    for (int s = 0; s < DS; ++s) {
+        sA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds16(ldsK + kofs[s]), qf[s], sA, 0, 0, 0);
+        sB = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds16(ldsK + CHUNK_B + kofs[s]), qf[s], sB, 0, 0, 0);
+    }
+    bf16x8 pA0, pA1, pB0, pB1;                     // weights of even / odd chunks
+    finish(sA, key_of(0));
+    raise(sA, pA0, pA1);
+
+    Pages pg2 = pages_of(2);
+    // tile t = steps 2t and 2t + 1: reads K(t + 1) (logits ahead) and V^T(t)
+    auto one_tile = [&](auto par_tag, int t) {
+        constexpr int PAR = decltype(par_tag)::value;      // t % 2
+        using KB = IC<1 - PAR>;
+        using VB = IC<PAR>;
+        if (t > 0) {                                       // K(t + 1) and V^T(t) have been requested
+            wait_for_loads();
+            clear_unseen(VB{}, t);
+        }
+        __syncthreads();                                   // they are there, and the buffers refilled below have been read
+        bf16x8 f[4];
+        f[0] = lds16(ldsK + KB::value * TILE_B + kofs[0]);
+        f[1] = lds16(ldsV + VB::value * TILE_B + vofs[0]);
+        f[2] = lds16(ldsK + KB::value * TILE_B + kofs[1]);
+        if (t + 2 < n_st) issue_k(IC<PAR>{}, t + 2, pg2);
+        if (t + 1 < n_st) issue_v(IC<1 - PAR>{}, t + 1, pg1);
+        pg1 = pg2;
+        pg2 = pages_of(t + 3);
+        const bool on = 2 * t <= last_chunk, on2 = 2 * t + 1 <= last_chunk;
+        if (on) {
+            finish(sB, key_of(t) + 32);
+            step(KB{}, VB{}, IC<0>{}, sB, sA, pA0, pA1, pB0, pB1, f);
+        }
+        if (on2) {
+            if (t + 1 >= n_st) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sA[r] = -INFINITY;        // past the end: logits of a stale buffer
+            } else {
+                finish(sA, key_of(t + 1));
+            }
+            step(KB{}, VB{}, IC<1>{}, sA, sB, pB0, pB1, pA0, pA1, f);
+        }
+    };
+    for (int t = 0;;) {
+        one_tile(IC<0>{}, t);
+        if (++t == n_st) break;
+        one_tile(IC<1>{}, t);
+        if (++t == n_st) break;
+    }
+
+    const float lt = l + other_half(l);
+    const bool none = m == -INFINITY && lt == 0.f;         // a row that sees no key; NaN is not none
+    const float inv = none ? 0.f : 1.f / lt;
+    const float lse2 = none ? -INFINITY : mc + __log2f(lt);
+    if (!valid) return;
+    if (partial) {
+#pragma unroll
+        for (int dc = 0; dc < DT; ++dc)
+#pragma unroll
+            for (int rq = 0; rq < 4; ++rq) {
+                f32x4 o4;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o4[x] = oacc[dc][4 * rq + x] * inv;
+                *reinterpret_cast<f32x4*>(po + 32 * dc + 8 * rq + 4 * half) = o4;
+            }
+        if (half == 0) *plse = lse2;
+    } else {
+#pragma unroll
+        for (int dc = 0; dc < DT; ++dc)
+#pragma unroll
+            for (int rq = 0; rq < 4; ++rq) {
+                f32x4 o4;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o4[x] = oacc[dc][4 * rq + x] * inv;
+                *reinterpret_cast<bf16x4*>(orow + 32 * dc + 8 * rq + 4 * half) = __builtin_convertvector(o4, bf16x4);
+            }
+        if (a.lse != nullptr && half == 0) a.lse[(int64_t)(sh.r.first + token) * a.Hq + head] = lse2 * kLn2;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
 // Merge of the pieces' results: one workgroup for 16 rows, a wavefront per row, D / 8 lanes a piece.
 template <int D>
 __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& part, uint32_t item) {
@@ -435,7 +801,8 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a, PagedPart
 // Most workgroups of a part that a call can need, whatever its lengths (below `target` more than without cuts, and none
 // cut into pieces of less than min_tiles)
 int64_t most_units(const PagedDims& d, const PagedPart& part) {
-    const int64_t tiles = ((int64_t)d.T * d.G / part.m + (d.B < d.T ? d.B : d.T)) * d.Hkv;
+    const int64_t requests = d.B < d.T ? d.B : d.T;
+    const int64_t tiles = (part.row_hi <= part.m ? requests : (int64_t)d.T * d.G / part.m + requests) * d.Hkv;
     const int64_t keys = (((int64_t)d.C << d.log_p) + kPagedTile - 1) / kPagedTile;
     const int64_t cuts = (keys + part.min_tiles - 1) / part.min_tiles;
     const int64_t target = 1ll << part.log_target;
@@ -474,6 +841,22 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
         if (e != hipSuccess) return e;
         few_merges = parts.few.n_slots / 2 * (parts.few.m / 16);        // a row tile that is cut has two pieces at least
     }
+    if (parts.many.m) {
+        const int64_t grid = most_units(d, parts.many);
+        if (grid > 0x7fffffffll) return hipErrorInvalidValue;
+        const bool mod = a.cap > 0.f || a.slopes != nullptr;
+        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, st, a, parts.many); };
+        if (a.log_p < 6) {
+            if (mod) go(paged_many_kernel<D, true, true>);
+            else go(paged_many_kernel<D, false, true>);
+        } else {
+            if (mod) go(paged_many_kernel<D, true, false>);
+            else go(paged_many_kernel<D, false, false>);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        many_merges = parts.many.n_slots / 2 * (kManyRows / 16);
+    }
     if (few_merges + many_merges == 0) return hipSuccess;
     hipLaunchKernelGGL((paged_merge_kernel<D>), dim3((unsigned)(few_merges + many_merges)), dim3(256), 0, st, a, parts.few, parts.many,
                        (unsigned)few_merges);
@@ -484,13 +867,29 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
 
 PagedParts paged_parts(const PagedDims& d, void* ws_or_null) {
     PagedParts p{};
-    p.few.m = d.G <= 16 && (d.max_new == 0 || (int64_t)d.max_new * d.G <= 16 || d.B > 1) ? 16 : 32;
-    p.few.log_m = p.few.m == 16 ? 4 : 5;
-    p.few.span = (p.few.m + d.G - 1) / d.G + 1;
-    p.few.log_target = 11;
-    p.few.min_tiles = 4;
-    p.few.row_lo = 0;
-    p.few.row_hi = 0x7fffffff;
+    const int most_new = d.max_new > 0 && d.max_new < d.T ? d.max_new : d.T;
+    const int64_t most_rows = (int64_t)most_new * d.G;
+    // Few rows are bound by the loads of keys and values, many by the matrix products: up to 32 rows go to the one kernel,
+    // more to the other.  Both are launched where a call may have requests of both kinds.
+    const int few_rows = most_rows <= 16 || (most_rows > 32 && d.G <= 16) ? 16 : 32;
+    if (most_rows <= few_rows || (d.B > 1 && d.G <= few_rows)) {
+        p.few.m = few_rows;
+        p.few.log_m = few_rows == 16 ? 4 : 5;
+        p.few.span = (p.few.m + d.G - 1) / d.G + 1;
+        p.few.log_target = 11;
+        p.few.min_tiles = 4;
+        p.few.row_lo = 0;
+        p.few.row_hi = most_rows <= few_rows ? 0x7fffffff : few_rows;
+    }
+    if (most_rows > few_rows) {
+        p.many.m = kManyRows;
+        p.many.log_m = 7;
+        p.many.span = (p.many.m + d.G - 1) / d.G + 1;
+        p.many.log_target = 9;
+        p.many.min_tiles = 8;
+        p.many.row_lo = p.few.m ? few_rows : 0;
+        p.many.row_hi = 0x7fffffff;
+    }
     size_t off = 0;
     for (PagedPart* part : {&p.few, &p.many}) {
         if (part->m == 0) continue;
