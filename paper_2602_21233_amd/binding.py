@@ -95,11 +95,11 @@ def load_library():
     lib.sparse_prefill_select_ex.argtypes = [pp, vp, vp, po, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.sparse_prefill_topk_from_scores_ex.argtypes = [pp, vp, po, vp, vp, vp]
     lib.sparse_prefill_fused_ex.argtypes = [pp, vp, vp, vp, po, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
-    pg = ctypes.POINTER(SpaPagedParams)
-    lib.spa_paged_workspace_bytes.argtypes = [pg, ctypes.POINTER(ctypes.c_size_t)]
-    lib.sparse_prefill_paged_plan.argtypes = [pg, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp, vp, vp, vp]
-    lib.sparse_prefill_paged_append.argtypes = [pg, vp, vp, vp, vp, vp, vp]
-    lib.sparse_prefill_paged_attn.argtypes = [pg, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    # the paged calls take their parameters as packed bytes, or by reference
+    lib.spa_paged_workspace_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
+    lib.sparse_prefill_paged_plan.argtypes = [vp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sparse_prefill_paged_append.argtypes = [vp, vp, vp, vp, vp, vp, vp]
+    lib.sparse_prefill_paged_attn.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     for name in EXPORTS[1:]:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib

@@ -79,11 +79,10 @@ struct Share {
     PagedShare s;
     Request r;
 };
-// MERGE: units are those of the merge kernel, m / 16 for each (row tile, KV head) of a request whose keys are cut
+// MERGE: units are the rows of requests whose keys are cut, KV heads next to each other
 template <bool MERGE>
-__device__ __forceinline__ Share share_of_workgroup(const PagedArgs& a, const PagedPart& part, uint32_t item) {
+__device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedPart& part, int piece, uint32_t item) {
     const int lane = threadIdx.x & 63;
-    const int piece = part_piece(a, part, lane);
     uint32_t items_before = 0, slots_before = 0;
     Share found;
     found.b = -1;
@@ -92,7 +91,7 @@ __device__ __forceinline__ Share share_of_workgroup(const PagedArgs& a, const Pa
         const PagedShare s = share_at(a, part, r, piece);
         const uint32_t units = (uint32_t)s.tiles * (uint32_t)s.splits * (uint32_t)a.Hkv;
         const uint32_t slots = s.splits > 1 ? units : 0u;
-        const uint32_t items = !MERGE ? units : (s.splits > 1 ? (uint32_t)s.tiles * (uint32_t)a.Hkv * (uint32_t)(part.m / 16) : 0u);
+        const uint32_t items = !MERGE ? units : (s.splits > 1 ? (uint32_t)(r.len * a.Hq) : 0u);
         const uint32_t items_upto = items_before + wave_scan(items), slots_upto = slots_before + wave_scan(slots);
         const uint64_t here = __ballot(item >= items_upto - items && item < items_upto);
         if (here != 0) {
@@ -109,6 +108,9 @@ __device__ __forceinline__ Share share_of_workgroup(const PagedArgs& a, const Pa
         slots_before = last_lane(slots_upto);
     }
     return found;
+}
+__device__ __forceinline__ Share share_of_workgroup(const PagedArgs& a, const PagedPart& part) {
+    return share_of<false>(a, part, part_piece(a, part, threadIdx.x & 63), blockIdx.x);
 }
 // a request's key tiles are dealt to its pieces evenly
 __device__ __forceinline__ int tiles_of_piece(const PagedShare& s) { return (int)((uint32_t)(s.keys + s.splits - 1) / (uint32_t)s.splits); }
@@ -162,7 +164,7 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs a, PagedPar
     __shared__ __attribute__((aligned(16))) float s_o[NW][16][PAD];
     __shared__ float s_m[NW][MF * 16], s_l[NW][MF * 16];
 
-    const Share sh = share_of_workgroup<false>(a, part, blockIdx.x);
+    const Share sh = share_of_workgroup(a, part);
     if (sh.b < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4;
@@ -391,7 +393,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
     __shared__ __attribute__((aligned(1024))) uint16_t smemK[2][TILE];
     __shared__ __attribute__((aligned(1024))) uint16_t smemV[2][TILE];
 
-    const Share sh = share_of_workgroup<false>(a, part, blockIdx.x);
+    const Share sh = share_of_workgroup(a, part);
     if (sh.b < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, l32 = lane & 31;
@@ -727,59 +729,63 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Merge of the pieces' results: one workgroup for 16 rows, a wavefront per row, D / 8 lanes a piece.
+// Merge of the pieces' results, a wavefront per row: out = sum_s w_s out_s / sum_s w_s, w_s = 2^(lse_s - max).  64 pieces at a time: a
+// lane has the weight of one, then D / 8 lanes read a piece's values, 64 / (D / 8) pieces side by side.
 template <int D>
-__device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& part, uint32_t item) {
-    constexpr int LPR = D / 8, NG = 64 / LPR;       // lanes of a piece, pieces at a time
-    const Share sh = share_of_workgroup<true>(a, part, item);
-    if (sh.b < 0) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int subs = part.m / 16;
-    const int sub = sh.unit % subs, u = sh.unit / subs;
-    const int kvh = u % a.Hkv, rank = u / a.Hkv;    // rank: row tiles from the last one on
-    const int rows = sh.r.len * a.G;
-    const int splits = sh.s.splits;
-    const int slot0 = sh.slot + rank * splits * a.Hkv + kvh;
-    if (slot0 + (splits - 1) * a.Hkv >= part.n_slots) return;
-    for (int r = wave; r < 16; r += 4) {
-        const int rt = 16 * sub + r, row = (sh.s.tiles - 1 - rank) * part.m + rt;
-        if (row >= rows) continue;
-        const float* lse = part.lse + rt;
-        float mx = -INFINITY;
-        bool bad = false;                           // NaN somewhere: fmaxf drops it
-        for (int s = lane; s < splits; s += 64) {
-            const float v = lse[(int64_t)(slot0 + s * a.Hkv) * part.m];
-            bad |= v != v;
-            mx = fmaxf(mx, v);
-        }
-#pragma unroll
-        for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
-        const int d0 = 8 * (lane % LPR);
-        float acc[8], total = 0.f;
+__device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& part) {
+    constexpr int LPR = D / 8, NG = 64 / LPR;       // lanes of a piece, pieces side by side
+    const int lane = threadIdx.x & 63;
+    const int grp = lane / LPR, d0 = 8 * (lane % LPR);
+    const int piece = part_piece(a, part, lane);
+    for (uint32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);; item += gridDim.x * 4) {
+        const Share sh = share_of<true>(a, part, piece, (uint32_t)__builtin_amdgcn_readfirstlane((int)item));
+        if (sh.b < 0) return;
+        const int kvh = sh.unit % a.Hkv, row = sh.unit / a.Hkv, splits = sh.s.splits;
+        const int tile = row >> part.log_m, rt = row & (part.m - 1);
+        const int slot0 = sh.slot + (sh.s.tiles - 1 - tile) * splits * a.Hkv + kvh;
+        if (slot0 + (splits - 1) * a.Hkv >= part.n_slots) continue;
+        auto at = [&](int s) { return (int64_t)(slot0 + s * a.Hkv) * part.m + rt; };
+        float mx = -INFINITY, total = 0.f, acc[8];
 #pragma unroll
         for (int x = 0; x < 8; ++x) acc[x] = 0.f;
-        if (mx != -INFINITY || __any(bad)) {
-            for (int s = lane / LPR; s < splits; s += NG) {
-                const int64_t at = (int64_t)(slot0 + s * a.Hkv) * part.m;
-                const float v = lse[at];
-                if (v == -INFINITY) continue;       // an empty piece; its sums may not have been written
-                const float w = __builtin_amdgcn_exp2f(v - mx);
-                const f32x4* po = reinterpret_cast<const f32x4*>(part.o + (at + rt) * D + d0);
-                const f32x4 p0 = po[0], p1 = po[1];
-                total += w;
+        for (int s0 = 0; s0 < splits; s0 += 64) {
+            const float v = s0 + lane < splits ? part.lse[at(s0 + lane)] : -INFINITY;
+            float top = v;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    acc[x] = fmaf(p0[x], w, acc[x]);
-                    acc[4 + x] = fmaf(p1[x], w, acc[4 + x]);
+            for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));     // NaN is dropped here and comes back with the weights
+            const float mx_new = fmaxf(mx, top);
+            const float old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - mx_new);
+            mx = mx_new;
+            const float w = v == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(v - mx);
+            total = fmaf(total, old, w);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) acc[x] *= old;
+            const int n = min(64, splits - s0);
+            for (int s = 0; s < n; s += 4 * NG) {           // four loads of a lane in flight
+                float ws[4];
+                f32x4 p[4][2];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int mine = s + NG * y + grp, there = min(mine, n - 1);
+                    const float wy = __shfl(w, there);
+                    ws[y] = mine < n ? wy : 0.f;
+                    const f32x4* const po = reinterpret_cast<const f32x4*>(part.o + at(s0 + there) * D + d0);
+                    p[y][0] = po[0];
+                    p[y][1] = po[1];
                 }
-            }
 #pragma unroll
-            for (int x = LPR; x < 64; x <<= 1) {
-                total += __shfl_xor(total, x);
+                for (int y = 0; y < 4; ++y)
 #pragma unroll
-                for (int y = 0; y < 8; ++y) acc[y] += __shfl_xor(acc[y], x);
+                    for (int x = 0; x < 8; ++x)             // a piece without a key in sight may not have written its values
+                        acc[x] = ws[y] != 0.f ? fmaf(p[y][x >> 2][x & 3], ws[y], acc[x]) : acc[x];
             }
         }
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) total += __shfl_xor(total, x);
+#pragma unroll
+        for (int x = LPR; x < 64; x <<= 1)
+#pragma unroll
+            for (int y = 0; y < 8; ++y) acc[y] += __shfl_xor(acc[y], x);
         const bool none = total == 0.f;
         const float inv = none ? 0.f : 1.f / total;
         if (lane < LPR) {
@@ -793,9 +799,9 @@ __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& 
     }
 }
 template <int D>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a, PagedPart few, PagedPart many, unsigned few_grid) {
-    if (blockIdx.x < few_grid) merge_rows<D>(a, few, blockIdx.x);
-    else merge_rows<D>(a, many, blockIdx.x - few_grid);
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a, PagedPart few, PagedPart many) {
+    if (few.n_slots > 0) merge_rows<D>(a, few);
+    if (many.n_slots > 0) merge_rows<D>(a, many);
 }
 
 // Most workgroups of a part that a call can need, whatever its lengths (below `target` more than without cuts, and none
@@ -831,7 +837,6 @@ void launch_few(const PagedArgs& a, const PagedPart& part, unsigned grid, hipStr
 
 template <int D>
 hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts& parts, hipStream_t st) {
-    int64_t few_merges = 0, many_merges = 0;
     if (parts.few.m) {
         const int64_t grid = most_units(d, parts.few);
         if (grid > 0x7fffffffll) return hipErrorInvalidValue;
@@ -839,7 +844,6 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
         else launch_few<D, 2>(a, parts.few, (unsigned)grid, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        few_merges = parts.few.n_slots / 2 * (parts.few.m / 16);        // a row tile that is cut has two pieces at least
     }
     if (parts.many.m) {
         const int64_t grid = most_units(d, parts.many);
@@ -855,11 +859,10 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        many_merges = parts.many.n_slots / 2 * (kManyRows / 16);
     }
-    if (few_merges + many_merges == 0) return hipSuccess;
-    hipLaunchKernelGGL((paged_merge_kernel<D>), dim3((unsigned)(few_merges + many_merges)), dim3(256), 0, st, a, parts.few, parts.many,
-                       (unsigned)few_merges);
+    if (parts.few.n_slots + parts.many.n_slots == 0) return hipSuccess;
+    const int64_t rows = ((int64_t)d.T * d.Hq + 3) / 4;
+    hipLaunchKernelGGL((paged_merge_kernel<D>), dim3((unsigned)(rows < 1024 ? rows : 1024)), dim3(256), 0, st, a, parts.few, parts.many);
     return hipGetLastError();
 }
 
@@ -877,7 +880,7 @@ PagedParts paged_parts(const PagedDims& d, void* ws_or_null) {
         p.few.log_m = few_rows == 16 ? 4 : 5;
         p.few.span = (p.few.m + d.G - 1) / d.G + 1;
         p.few.log_target = 11;
-        p.few.min_tiles = 4;
+        p.few.min_tiles = 8;
         p.few.row_lo = 0;
         p.few.row_hi = most_rows <= few_rows ? 0x7fffffff : few_rows;
     }

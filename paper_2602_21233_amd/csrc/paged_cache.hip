@@ -25,14 +25,16 @@ __device__ __forceinline__ uint32_t scan_capped(uint32_t v) {
 // tokens of its own: one launch, nothing handed from one workgroup to another.  A page that the step takes starts at one of
 // its new tokens, so the token at a page's start also writes the table entry.  Bound by latency at every size that occurs.
 constexpr int kPlanThreads = 256;
-constexpr int kPlanTokens = 4 * kPlanThreads;      // tokens of a workgroup
+constexpr int kFewAppended = 1024;                 // tokens up to which paged_append_kernel moves them
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(
     const int32_t* __restrict__ ctx_lens, const int32_t* __restrict__ new_lens, const int32_t* __restrict__ free_pages, int n_free,
     const int32_t* __restrict__ free_range, int32_t* __restrict__ table, int64_t table_stride, int32_t* __restrict__ q_starts,
     int32_t* __restrict__ kv_lens, int32_t* __restrict__ slots, int32_t* __restrict__ positions, int32_t* __restrict__ taken, int B, int C,
     int T, int log_p, int n_pages) {
-    __shared__ int32_t s_start[kMaxRequests + 1];
-    __shared__ int32_t s_before[kMaxRequests];     // pages taken by the requests before; -1: left out
+    extern __shared__ int32_t s_requests[];        // 3 B + 1
+    int32_t* const s_start = s_requests;
+    int32_t* const s_before = s_start + B + 1;     // pages taken by the requests before; -1: left out
+    int32_t* const s_ctx = s_before + B;
     __shared__ uint32_t s_sum[2][2][kPlanThreads / 64];
     __shared__ int32_t s_taken, s_left_out;
 
@@ -72,6 +74,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(
         if (b < B) {
             s_start[b] = (int)min(start, (uint32_t)T);
             s_before[b] = goes ? (int)(upto - need) : -1;
+            s_ctx[b] = ctx;
             if (b == B - 1) s_start[B] = (int)min(end, (uint32_t)T);
             if (first_wg) {
                 q_starts[b] = (int)min(start, (uint32_t)T);
@@ -88,7 +91,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(
         taken[1] = s_left_out;
     }
 
-    for (int t = blockIdx.x * kPlanTokens + tid; t < min(T, (int)(blockIdx.x + 1) * kPlanTokens); t += kPlanThreads) {
+    for (int t = blockIdx.x * kPlanThreads + tid; t < T; t += gridDim.x * kPlanThreads) {
         int slot = -1, pos = 0;
         if (t < s_start[B]) {
             int lo = 0, hi = B;                    // the last request that starts at or before t: s_start[lo] <= t < s_start[hi]
@@ -97,7 +100,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(
                 if (s_start[mid] <= t) lo = mid;
                 else hi = mid;
             }
-            const int ctx = ctx_lens[lo], before = s_before[lo];
+            const int ctx = s_ctx[lo], before = s_before[lo];
             pos = (int)((uint32_t)ctx + (uint32_t)(t - s_start[lo]));
             if (before >= 0) {
                 const int col = pos >> log_p, have = (ctx + page - 1) >> log_p;
@@ -116,84 +119,153 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(
     }
 }
 
-// K and V of TT tokens of one head into their pages.  K rows are copied in 16-byte pieces.  V goes through LDS: where 8 tokens
-// that follow each other fill an aligned 16-byte piece of a page's rows (a prompt's tokens do, wherever its chunk starts), the
-// piece is stored whole, other tokens value by value.  HBM-bound: every value is read and written once.
-template <int D, int TT>
+__device__ __forceinline__ int64_t place_of(int slot, int log_p, int64_t page_stride, int in_page) {
+    return (slot >> log_p) * page_stride + (int64_t)(slot & ((1 << log_p) - 1)) * in_page;
+}
+
+// Few tokens: a thread moves 8 dims of one token, V in single values.  Bound by latency.
+template <int D>
 __global__ __launch_bounds__(256) void paged_append_kernel(const uint16_t* __restrict__ k, int64_t k_t, int64_t k_h, const uint16_t* __restrict__ v,
                                                            int64_t v_t, int64_t v_h, const int32_t* __restrict__ slots, uint16_t* __restrict__ k_pages,
                                                            int64_t kp_p, int64_t kp_h, uint16_t* __restrict__ vt_pages, int64_t vp_p, int64_t vp_h,
                                                            int T, int log_p, int n_slots, int Hkv) {
-    constexpr int CPR = D / 8;                     // 16-byte pieces of a row
-    constexpr int PAD = D + 8;
-    __shared__ __attribute__((aligned(16))) uint16_t s_v[TT][PAD];
-    __shared__ int32_t s_slot[TT];
-    __shared__ int32_t s_run[TT / 8 + 1], s_one[TT];   // first tokens of whole pieces; tokens stored one by one
-    __shared__ int32_t s_runs, s_ones;
+    constexpr int CPR = D / 8;
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int c = (int)(u % CPR), h = (int)(u / CPR % Hkv);
+    const int64_t t = u / CPR / Hkv;
+    if (t >= T) return;
+    const uint4 kr = *reinterpret_cast<const uint4*>(k + t * k_t + h * k_h + 8 * c);
+    const uint4 vr = *reinterpret_cast<const uint4*>(v + t * v_t + h * v_h + 8 * c);
+    const int s = slots[t];
+    if (s < 0 || s >= n_slots) return;
+    *reinterpret_cast<uint4*>(k_pages + place_of(s, log_p, kp_p, D) + h * kp_h + 8 * c) = kr;
+    uint16_t* const at = vt_pages + place_of(s, log_p, vp_p, 1) + h * vp_h + ((int64_t)(8 * c) << log_p);
+    const uint32_t w[4] = {vr.x, vr.y, vr.z, vr.w};
+#pragma unroll
+    for (int x = 0; x < 8; ++x) at[x << log_p] = (uint16_t)(w[x >> 1] >> (16 * (x & 1)));
+}
 
-    const int tid = threadIdx.x;
-    const int h = blockIdx.x % Hkv, t0 = blockIdx.x / Hkv * TT;
-    const int n = min(TT, T - t0), page = 1 << log_p;
-    if (tid < TT) {
-        const int s = tid < n ? slots[t0 + tid] : -1;
-        s_slot[tid] = s >= 0 && s < n_slots ? s : -1;
-    }
-    if (tid == 0) { s_runs = 0; s_ones = 0; }
-    // the loads need no slot
-    constexpr int PT = TT * CPR / 256 > 0 ? TT * CPR / 256 : 1;   // pieces of a thread
-    uint4 kr[PT], vr[PT];
+// Many tokens: a wavefront moves 64 tokens x 64 dims of a head, a lane 8 tokens (a window) x 8 dims.  Where 8 tokens that follow
+// each other fill an aligned 16-byte piece of a page's V rows (those of a prompt do, wherever its chunk starts), the lane that has
+// the first of them in its window loads all 8, transposes them in registers and stores the pieces whole; the tokens before the
+// first piece of a prompt and behind its last one are stored value by value.  All loads of a lane are in flight at once.
+// HBM-bound: every value is read and written once.
+template <int D>
+__global__ __launch_bounds__(256) void paged_append_runs_kernel(const uint16_t* __restrict__ k, int64_t k_t, int64_t k_h, const uint16_t* __restrict__ v,
+                                                                int64_t v_t, int64_t v_h, const int32_t* __restrict__ slots,
+                                                                uint16_t* __restrict__ k_pages, int64_t kp_p, int64_t kp_h,
+                                                                uint16_t* __restrict__ vt_pages, int64_t vp_p, int64_t vp_h, int T, int log_p, int n_slots,
+                                                                int Hkv, int64_t n_units) {
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (unit >= n_units) return;
+    const int c = 8 * (lane & 7) + 64 * (int)(unit % (D / 64));      // first of the lane's 8 dims
+    const int h = (int)(unit / (D / 64) % Hkv), t0 = (int)(unit / (D / 64) / Hkv) * 64;
+    const int window = 8 * (lane >> 3);
+
+    // The slots of tokens t0 - 8 .. t0 + 71: token t0 - 8 + lane in `early`, t0 + 56 + lane in `late`; -1 where there is none.
+    auto slot_at = [&](int t) {
+        const int s = t >= 0 && t < T ? slots[t] : -1;
+        return s >= 0 && s < n_slots ? s : -1;
+    };
+    const int early = slot_at(t0 - 8 + lane), late = slot_at(t0 + 56 + lane);
+    auto slot_of = [&](int i) {                                      // of token t0 + i, -8 <= i < 72
+        const int x = __shfl(early, (i + 8) & 63), y = __shfl(late, (i - 56) & 63);
+        return i < 56 ? x : y;
+    };
+    // bit i: 8 tokens from token t0 - 8 + i on (i < 64), or from t0 + i - 8 on for the last ones, make a whole piece
+    bool whole = true, whole_end = true;
+    const int head = early, tail = slot_of(56 + (lane & 7));
+    whole &= head >= 0 && (head & 7) == 0;
+    whole_end &= tail >= 0 && (tail & 7) == 0;
 #pragma unroll
-    for (int x = 0; x < PT; ++x) {
-        const int u = tid + 256 * x, row = u / CPR, c = u % CPR;
-        if (row < n) {
-            kr[x] = *reinterpret_cast<const uint4*>(k + (t0 + row) * k_t + h * k_h + 8 * c);
-            vr[x] = *reinterpret_cast<const uint4*>(v + (t0 + row) * v_t + h * v_h + 8 * c);
+    for (int x = 1; x < 8; ++x) {
+        whole &= slot_of(lane - 8 + x) == head + x;
+        whole_end &= slot_of(56 + (lane & 7) + x) == tail + x;
+    }
+    const uint64_t before = __ballot(whole);                         // starts t0 - 8 .. t0 + 55
+    const uint64_t last8 = __ballot(whole_end) & 0xff;               // starts t0 + 56 .. t0 + 63
+    const uint64_t starts = (before >> 8) | (last8 << 56);           // starts t0 .. t0 + 63
+    uint64_t covered = 0;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) covered |= (starts << x) | ((before & 0xff) << x >> 8);
+
+    const int mine = (int)(starts >> window) & 0xff;                 // pieces are disjoint, so at most one starts in a window
+    const int first = window + (mine != 0 ? __builtin_ctz(mine) : 0);
+    const uint16_t* const vh = v + h * v_h + c;
+    const uint16_t* const kh = k + h * k_h + c;
+    uint4 kr[8], vr[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+        kr[x] = *reinterpret_cast<const uint4*>(kh + (int64_t)min(t0 + window + x, T - 1) * k_t);
+        vr[x] = *reinterpret_cast<const uint4*>(vh + (int64_t)min(t0 + first + x, T - 1) * v_t);
+    }
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+        const int s = slot_of(window + x);
+        if (s >= 0) *reinterpret_cast<uint4*>(k_pages + place_of(s, log_p, kp_p, D) + h * kp_h + c) = kr[x];
+    }
+    const int s0 = slot_of(first);
+    uint16_t* const vth = vt_pages + h * vp_h + ((int64_t)c << log_p);
+    auto store_one = [&](int s, const uint4& r) {
+        uint16_t* const at = vth + place_of(s, log_p, vp_p, 1);
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int y = 0; y < 8; ++y) at[y << log_p] = (uint16_t)(w[y >> 1] >> (16 * (y & 1)));
+    };
+    // -1 for tokens of a whole piece
+    int single[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+        const int s = slot_of(window + x);
+        single[x] = (covered >> (window + x)) & 1 ? -1 : s;
+    }
+    if (mine != 0) {
+        uint16_t* const at = vth + place_of(s0, log_p, vp_p, 1);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {                                // dims c + 2p and c + 2p + 1
+            uint32_t in[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) in[x] = p == 0 ? vr[x].x : p == 1 ? vr[x].y : p == 2 ? vr[x].z : vr[x].w;
+            uint32_t lo[4], hi[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                lo[x] = __builtin_amdgcn_perm(in[2 * x + 1], in[2 * x], 0x05040100u);
+                hi[x] = __builtin_amdgcn_perm(in[2 * x + 1], in[2 * x], 0x07060302u);
+            }
+            *reinterpret_cast<uint4*>(at + ((int64_t)(2 * p) << log_p)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            *reinterpret_cast<uint4*>(at + ((int64_t)(2 * p + 1) << log_p)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         }
-    }
-    __syncthreads();
-    if (tid < TT && s_slot[tid] >= 0) {
-        const int lead = tid - (s_slot[tid] & 7);  // the token that would start this one's piece
-        bool whole = lead >= 0 && lead + 7 < n;
-        if (whole) {
-            const int s = s_slot[tid] & ~7;
+        for (int x = 0; window + x < first; ++x) {                   // tokens of the window before its piece
+            int s = -1;
 #pragma unroll
-            for (int x = 0; x < 8; ++x) whole &= s_slot[lead + x] == s + x;
+            for (int y = 0; y < 8; ++y) s = y == x ? single[y] : s;
+            if (s >= 0) store_one(s, *reinterpret_cast<const uint4*>(vh + (int64_t)(t0 + window + x) * v_t));
         }
-        if (whole && lead == tid) s_run[atomicAdd(&s_runs, 1)] = tid;
-        if (!whole) s_one[atomicAdd(&s_ones, 1)] = tid;
-    }
+    } else {
 #pragma unroll
-    for (int x = 0; x < PT; ++x) {
-        const int u = tid + 256 * x, row = u / CPR, c = u % CPR;
-        if (row < n) {
-            *reinterpret_cast<uint4*>(&s_v[row][8 * c]) = vr[x];
-            const int s = s_slot[row];
-            if (s >= 0) *reinterpret_cast<uint4*>(k_pages + (s >> log_p) * kp_p + h * kp_h + (s & (page - 1)) * D + 8 * c) = kr[x];
-        }
-    }
-    __syncthreads();
-    const int runs = s_runs, ones = s_ones;
-    for (int u = tid; u < runs * D; u += 256) {
-        const int d = u / runs, i = s_run[u % runs], s = s_slot[i];
-        uint16_t w[8];
-#pragma unroll
-        for (int x = 0; x < 8; ++x) w[x] = s_v[i + x][d];
-        *reinterpret_cast<uint4*>(vt_pages + (s >> log_p) * vp_p + h * vp_h + (int64_t)d * page + (s & (page - 1))) = *reinterpret_cast<const uint4*>(w);
-    }
-    for (int u = tid; u < ones * D; u += 256) {
-        const int d = u / ones, i = s_one[u % ones], s = s_slot[i];
-        vt_pages[(s >> log_p) * vp_p + h * vp_h + (int64_t)d * page + (s & (page - 1))] = s_v[i][d];
+        for (int x = 0; x < 8; ++x)
+            if (single[x] >= 0) store_one(single[x], vr[x]);
     }
 }
 
-template <int D, int TT>
+template <int D>
 hipError_t launch_append(const PagedDims& d, const void* k, int64_t k_t, int64_t k_h, const void* v, int64_t v_t, int64_t v_h,
                          const int32_t* slots, void* k_pages, void* vt_pages, hipStream_t st) {
-    const int64_t nwg = (int64_t)((d.T + TT - 1) / TT) * d.Hkv;
-    if (nwg > 0x7fffffffll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((paged_append_kernel<D, TT>), dim3((unsigned)nwg), dim3(256), 0, st, (const uint16_t*)k, k_t, k_h, (const uint16_t*)v,
-                       v_t, v_h, slots, (uint16_t*)k_pages, d.kp_p, d.kp_h, (uint16_t*)vt_pages, d.vp_p, d.vp_h, d.T, d.log_p,
-                       d.n_pages << d.log_p, d.Hkv);
+    if (d.T <= kFewAppended) {
+        const int64_t nwg = ((int64_t)d.T * d.Hkv * (D / 8) + 255) / 256;
+        if (nwg > 0x7fffffffll) return hipErrorInvalidValue;
+        hipLaunchKernelGGL((paged_append_kernel<D>), dim3((unsigned)nwg), dim3(256), 0, st, (const uint16_t*)k, k_t, k_h, (const uint16_t*)v, v_t,
+                           v_h, slots, (uint16_t*)k_pages, d.kp_p, d.kp_h, (uint16_t*)vt_pages, d.vp_p, d.vp_h, d.T, d.log_p, d.n_pages << d.log_p,
+                           d.Hkv);
+    } else {
+        const int64_t units = ((int64_t)d.T + 63) / 64 * d.Hkv * (D / 64);
+        const int64_t nwg = (units + 3) / 4;
+        if (nwg > 0x7fffffffll) return hipErrorInvalidValue;
+        hipLaunchKernelGGL((paged_append_runs_kernel<D>), dim3((unsigned)nwg), dim3(256), 0, st, (const uint16_t*)k, k_t, k_h, (const uint16_t*)v,
+                           v_t, v_h, slots, (uint16_t*)k_pages, d.kp_p, d.kp_h, (uint16_t*)vt_pages, d.vp_p, d.vp_h, d.T, d.log_p,
+                           d.n_pages << d.log_p, d.Hkv, units);
+    }
     return hipGetLastError();
 }
 
@@ -202,16 +274,16 @@ hipError_t launch_append(const PagedDims& d, const void* k, int64_t k_t, int64_t
 hipError_t launch_paged_plan(const PagedDims& d, const int32_t* ctx_lens, const int32_t* new_lens, const int32_t* free_pages, int n_free,
                              const int32_t* free_range, int32_t* block_table, int32_t* q_starts, int32_t* kv_lens, int32_t* slots,
                              int32_t* positions_or_null, int32_t* taken, hipStream_t st) {
-    const unsigned nwg = (unsigned)(((int64_t)d.T + kPlanTokens - 1) / kPlanTokens);
-    hipLaunchKernelGGL(paged_plan_kernel, dim3(nwg), dim3(kPlanThreads), 0, st, ctx_lens, new_lens, free_pages, n_free, free_range,
+    const int wgs = (d.T + kPlanThreads - 1) / kPlanThreads;       // 1024 at most: enough to fill the chip, and none scans for little
+    hipLaunchKernelGGL(paged_plan_kernel, dim3(wgs < 1024 ? wgs : 1024), dim3(kPlanThreads), (3 * d.B + 1) * sizeof(int32_t), st, ctx_lens, new_lens, free_pages, n_free, free_range,
                        block_table, d.table_stride, q_starts, kv_lens, slots, positions_or_null, taken, d.B, d.C, d.T, d.log_p, d.n_pages);
     return hipGetLastError();
 }
 
 hipError_t launch_paged_append(const PagedDims& d, const void* k, int64_t k_t, int64_t k_h, const void* v, int64_t v_t, int64_t v_h,
                                const int32_t* slots, void* k_pages, void* vt_pages, hipStream_t st) {
-    return d.D == 128 ? launch_append<128, 64>(d, k, k_t, k_h, v, v_t, v_h, slots, k_pages, vt_pages, st)
-                      : launch_append<64, 64>(d, k, k_t, k_h, v, v_t, v_h, slots, k_pages, vt_pages, st);
+    return d.D == 128 ? launch_append<128>(d, k, k_t, k_h, v, v_t, v_h, slots, k_pages, vt_pages, st)
+                      : launch_append<64>(d, k, k_t, k_h, v, v_t, v_h, slots, k_pages, vt_pages, st);
 }
 
 }  // namespace spa
