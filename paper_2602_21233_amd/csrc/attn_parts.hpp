@@ -93,9 +93,7 @@ __device__ __forceinline__ void group_mfma(const bf16x8& a, const bf16x8 (&qf)[D
 // The group's share of the softmax arithmetic of chunk n + 1: its 16 logits s_cur form two halves of
 // 8 (keys 0-15 / 16-31), each turned into weights pn over NG / 2 consecutive groups: scaled
 // differences (8 fma), powers of two (8 exp2), conversion to bf16, denominator.
-// SUM32: the denominator takes the weights as they are in fp32, otherwise as they are in bf16 (half the instructions; the
-// weights' rounding then cancels between numerator and denominator, but the log-sum-exp carries it).
-template <int g, int D, bool SUM32 = false>
+template <int g, int D>
 __device__ __forceinline__ void group_weights(const f32x16& s_cur, float c, float mcb, f32x8& e, bf16x8& pn0, bf16x8& pn1,
                                               float& l_new) {
     constexpr int NG = D / 8;
@@ -116,12 +114,6 @@ __device__ __forceinline__ void group_weights(const f32x16& s_cur, float c, floa
         else pn1 = __builtin_convertvector(e, bf16x8);
     };
     auto sum_and_test = [&]() {
-        if constexpr (SUM32) {
-#pragma unroll
-            for (int x = 0; x < 8; ++x) l_new += e[x];
-            if constexpr (g == NG - 1) asm volatile("" : "+v"(l_new));
-            return;
-        }
         const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
         const bf16x8 pw = first_half ? pn0 : pn1;
 #pragma unroll

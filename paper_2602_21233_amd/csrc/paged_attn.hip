@@ -362,7 +362,92 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs a, PagedPar
 // four share through LDS: the pipeline step of the sparse prefill's attention kernel (attn.hip: direct loads into a double
 // buffer, logits two 32-key chunks ahead of the second product, one barrier a tile), with pages in place of blocks, masks
 // where a tile needs them instead of in the last block, and logits that may be capped or biased.
+// The keys are taken from the last tile to the first: with a bias that falls with the distance a row then meets its largest
+// logits first and its reference hardly moves.
 constexpr int kManyRows = 128;
+
+enum Mode { kPlain, kSlopes, kCapped };        // scaled products; with a bias by distance; capped (and maybe biased)
+
+// What the running softmax of a wavefront needs of its row for a chunk: the weight of the product s in register r (key key0 +
+// 16 (r / 8) + 8 half + r % 8) is 2^(s c + bias(r)), or with a cap 2^(bias(r) - 2 cap2 / (1 + 2^(s k))), the same as
+// cap2 tanh(...) since tanh y = 1 - 2 / (1 + e^2y).  bias holds - m, the cap and the slope's share.
+template <int MODE>
+struct ChunkWeights {
+    float c, k, cap2, slope2, base;
+    static __device__ __forceinline__ constexpr int key_of(int r) { return 16 * (r >> 3) + (r & 7); }
+    // ahead: position of register 0's key less the row's own.  The biases are counted from the lane's last key (r = 15): for keys
+    // that all lie at or before the row the two parts have one sign, so no precision is lost where a bias is small.
+    __device__ __forceinline__ void at(float m, int ahead) {
+        const float less_m = MODE == kCapped ? cap2 - m : -m;
+        base = MODE == kPlain ? less_m : fmaf(slope2, (float)(ahead + key_of(15)), less_m);
+    }
+    __device__ __forceinline__ float bias(int r) const { return MODE == kPlain ? base : fmaf(slope2, (float)(key_of(r) - key_of(15)), base); }
+    __device__ __forceinline__ float growth(float s) const { return __builtin_amdgcn_exp2f(s * k); }
+    // the exponent as a masked chunk needs it, where keys lie on both sides of the row
+    __device__ __forceinline__ float exponent(float s, int r, float m, int ahead) const {
+        const float less_m = MODE == kCapped ? cap2 - m : -m;
+        const float b = MODE == kPlain ? less_m : fmaf(slope2, (float)(ahead + key_of(r)), less_m);
+        if constexpr (MODE == kCapped) return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + growth(s)), b);
+        else return fmaf(s, c, b);
+    }
+};
+
+// Instruction group g of a step, its share of the softmax arithmetic: as group_weights (attn_parts.hpp), for all modes; the
+// denominator takes the weights in fp32, so that the log-sum-exp is as exact as the logits.
+template <int g, int D, int MODE>
+__device__ __forceinline__ void group_mode_weights(const f32x16& s, const ChunkWeights<MODE>& cw, f32x8& e, bf16x8& pn0, bf16x8& pn1, float& l_new) {
+    constexpr int NG = D / 8, HG = NG / 2;
+    constexpr int hb = (g / HG) * 8, gg = g % HG;
+    constexpr bool first_half = g < HG;
+    auto linear = [&](int x0, int n) {
+#pragma unroll
+        for (int x = x0; x < x0 + n; ++x) e[x] = fmaf(s[hb + x], cw.c, cw.bias(hb + x));
+    };
+    auto grow = [&](int x0, int n) {
+#pragma unroll
+        for (int x = x0; x < x0 + n; ++x) e[x] = cw.growth(s[hb + x]);
+    };
+    auto turn = [&](int x0, int n) {
+#pragma unroll
+        for (int x = x0; x < x0 + n; ++x) e[x] = __builtin_amdgcn_rcpf(1.f + e[x]);
+    };
+    auto capped = [&](int x0, int n) {
+#pragma unroll
+        for (int x = x0; x < x0 + n; ++x) e[x] = fmaf(-2.f * cw.cap2, e[x], cw.bias(hb + x));
+    };
+    auto exps = [&](int x0, int n) {
+#pragma unroll
+        for (int x = x0; x < x0 + n; ++x) e[x] = __builtin_amdgcn_exp2f(e[x]);
+    };
+    auto finish = [&]() {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) l_new += e[x];
+        if constexpr (first_half) pn0 = __builtin_convertvector(e, bf16x8);
+        else pn1 = __builtin_convertvector(e, bf16x8);
+        if constexpr (g == NG - 1) asm volatile("" : "+v"(l_new));   // keep the sums inside their groups
+    };
+    if constexpr (HG == 8 && MODE != kCapped) {
+        if constexpr (gg < 2) linear(4 * gg, 4);
+        else if constexpr (gg < 6) exps(2 * (gg - 2), 2);
+        else if constexpr (gg == 7) finish();
+    } else if constexpr (HG == 8) {
+        if constexpr (gg < 2) grow(4 * gg, 4);
+        else if constexpr (gg < 4) turn(4 * (gg - 2), 4);
+        else if constexpr (gg == 4) { capped(0, 8); exps(0, 1); }
+        else if constexpr (gg == 5) exps(1, 4);
+        else if constexpr (gg == 6) exps(5, 3);
+        else finish();
+    } else if constexpr (MODE != kCapped) {
+        if constexpr (gg == 0) linear(0, 8);
+        else if constexpr (gg < 3) exps(4 * (gg - 1), 4);
+        else finish();
+    } else {
+        if constexpr (gg == 0) grow(0, 8);
+        else if constexpr (gg == 1) turn(0, 8);
+        else if constexpr (gg == 2) { capped(0, 8); exps(0, 4); }
+        else { exps(4, 4); finish(); }
+    }
+}
 
 // 16 bytes per lane straight into LDS, each lane from an address of its own
 template <int IMM>
@@ -375,7 +460,7 @@ __device__ __forceinline__ void lds_dma16_from(uint32_t lds_addr, const void* la
 // this wavefront's direct loads have landed
 __device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-template <int D, bool MOD, bool SMALL>
+template <int D, int MODE, bool SMALL>
 __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPart part) {
     constexpr int NW = 4;
     constexpr int KT = kPagedTile;
@@ -434,7 +519,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
     const int32_t* const trow = a.table + (int64_t)sh.b * a.table_stride;
     const char* const kbase = reinterpret_cast<const char*>(a.k + kvh * a.kp_h);
     const char* const vbase0 = reinterpret_cast<const char*>(a.vt + kvh * a.vp_h);
-    auto key_of = [&](int t) { return kt.at(e0 + t) * KT; };                  // first key of tile t
+    auto key_of = [&](int t) { return kt.at(kt.n - 1 - e0 - t) * KT; };       // first key of tile t: the last tiles first
     auto page_of = [&](int key) { return clamp_int(trow[min(key >> a.log_p, last_col)], 0, a.n_pages - 1); };
     struct Pages {                                                            // of a tile's 16-key pieces (one page without SMALL)
         int id[SMALL ? 4 : 1];
@@ -529,7 +614,6 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
 #pragma unroll
         for (int s = 0; s < DS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qrow + 16 * s);
     }
-    const Logits lg = logits_of(a, head);
     int kofs[DS], vofs[4];
     {
         const int krow = swap_bits23(l32);
@@ -542,81 +626,80 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
     const char* const ldsV = reinterpret_cast<const char*>(&smemV[0][0]);
     auto lds16 = [](const char* p) { return *reinterpret_cast<const bf16x8*>(p); };
 
-    // Running softmax: weights 2^(x c - mc) of logits x, which are products as they come (c = scale * log2 e) or, with MOD, already
-    // in base 2 (c = 1).  m: the reference; -inf until the row has seen a key, and then limit = -1 sends it to the slow path.
+    // Running softmax, in base 2.  m: the reference; -inf until the row has seen a key, and then limit = -1 sends it to the slow path.
     f32x16 oacc[DT];
 #pragma unroll
     for (int dc = 0; dc < DT; ++dc)
 #pragma unroll
         for (int r = 0; r < 16; ++r) oacc[dc][r] = 0.f;
-    const float c = MOD ? 1.f : lg.c;
-    float m = -INFINITY, mc = 0.f, l = 0.f, limit = -1.f;
-    auto weights = [&](const f32x16& s, bf16x8& p0, bf16x8& p1) {
-        f32x8 w0, w1;
-        float sum = 0.f;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            w0[x] = __builtin_amdgcn_exp2f(fmaf(s[x], c, -mc));
-            w1[x] = __builtin_amdgcn_exp2f(fmaf(s[8 + x], c, -mc));
-        }
-#pragma unroll
-        for (int x = 0; x < 8; ++x) sum += w0[x];
-#pragma unroll
-        for (int x = 0; x < 8; ++x) sum += w1[x];
-        p0 = __builtin_convertvector(w0, bf16x8);
-        p1 = __builtin_convertvector(w1, bf16x8);
-        return sum;
+    ChunkWeights<MODE> cw;
+    cw.c = a.scale * kLog2e;
+    cw.cap2 = a.cap * kLog2e;
+    cw.k = MODE == kCapped ? 2.f * cw.c / a.cap : 0.f;
+    cw.slope2 = MODE != kPlain && a.slopes != nullptr ? a.slopes[head] * kLog2e : 0.f;
+    float m = -INFINITY, m0 = 0.f, l = 0.f, limit = -1.f;                     // m0: m, or 0 where that is -inf
+    const int wave_row = row0 + 32 * wave;                                    // wave-uniform bounds of this wavefront's rows
+    const int wave_lo = pos0 + min(wave_row, last_row) / a.G, wave_hi = pos0 + min(wave_row + 31, last_row) / a.G;
+    auto needs_mask = [&](int key0) {
+        return key0 + 31 > wave_lo || (a.window > 0 && key0 + 31 >= a.sink && key0 <= wave_hi - a.window);
     };
-    // moves the reference so that the chunk's weights are at most 1 and the denominator so far is about 1 or less
-    auto raise = [&](const f32x16& s, bf16x8& p0, bf16x8& p1) {
-        float mx = s[0];
+    // Slow path of a chunk: masks, and a reference that makes its weights at most 1 and the denominator so far about 1 or less.
+    // For the first chunk, masked ones, and where the denominator passed the limit.
+    auto slow_weights = [&](const f32x16& s, int key0, bf16x8& p0, bf16x8& p1) __attribute__((always_inline)) {
+        const int back = pos - key0 - 8 * half;
+        f32x16 x;
 #pragma unroll
-        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        for (int r = 0; r < 16; ++r) x[r] = cw.exponent(s[r], r, 0.f, -back);
+        uint32_t hidden = 0;
+        if (needs_mask(key0)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int b = back - 16 * (r >> 3) - (r & 7);
+                if (b < 0 || (a.window > 0 && b >= a.window && pos - b >= a.sink)) {
+                    hidden |= 1u << r;
+                    x[r] = -INFINITY;
+                }
+            }
+        }
+        float mx = x[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
         mx = fmaxf(mx, other_half(mx));
         const float lq = l + other_half(l);
         const bool first = m == -INFINITY;
-        const float m_new = fmaxf(first ? m : m + (lq > 1.f ? __log2f(lq) / c : 0.f), mx);
-        const float alpha = first ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * c);
+        const float m_new = fmaxf(first ? m : m + (lq > 1.f ? __log2f(lq) : 0.f), mx);
+        const float alpha = first ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
         m = m_new;
-        mc = m == -INFINITY ? 0.f : m * c;
+        m0 = m == -INFINITY ? 0.f : m;
         limit = m == -INFINITY ? -1.f : kRescaleAt;
         l *= alpha;
 #pragma unroll
         for (int dc = 0; dc < DT; ++dc)
 #pragma unroll
             for (int r = 0; r < 16; ++r) oacc[dc][r] *= alpha;
-        l += weights(s, p0, p1);
-    };
-
-    const int wave_row = row0 + 32 * wave;                                    // wave-uniform bounds of this wavefront's rows
-    const int wave_lo = pos0 + min(wave_row, last_row) / a.G, wave_hi = pos0 + min(wave_row + 31, last_row) / a.G;
-    // what options and masks make of a chunk's products; register r holds key key0 + 16 (r / 8) + 8 half + r % 8
-    auto finish = [&](f32x16& s, int key0) {
-        const int back = pos - key0 - 8 * half;
-        if constexpr (MOD) {
+        f32x8 w0, w1;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = logit<true>(lg, s[r], back - 16 * (r >> 3) - (r & 7));
+        for (int r = 0; r < 8; ++r) {
+            w0[r] = (hidden >> r) & 1 ? 0.f : __builtin_amdgcn_exp2f(cw.exponent(s[r], r, m0, -back));
+            w1[r] = (hidden >> (8 + r)) & 1 ? 0.f : __builtin_amdgcn_exp2f(cw.exponent(s[8 + r], 8 + r, m0, -back));
         }
-        if (key0 + 31 > wave_lo || (a.window > 0 && key0 + 31 >= a.sink && key0 <= wave_hi - a.window)) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int b = back - 16 * (r >> 3) - (r & 7);
-                if (b < 0 || (a.window > 0 && b >= a.window && pos - b >= a.sink)) s[r] = -INFINITY;
-            }
-        }
+        for (int r = 0; r < 8; ++r) l += w0[r] + w1[r];
+        p0 = __builtin_convertvector(w0, bf16x8);
+        p1 = __builtin_convertvector(w1, bf16x8);
     };
-    // last chunk with a key in sight of this wavefront; the steps behind it only load.  -1: it has no rows
-    int last_chunk = -1;
+    // first tile with a key in sight of this wavefront; two tiles and more before it, its steps would do nothing.  n_st + 1: no rows
+    int first_tile = n_st + 1;
     if (wave_row <= last_row && wave_hi >= 0) {
-        const int at = wave_hi / KT;
-        int e = at >= kt.from ? kt.sinks + at - kt.from : min(at, kt.sinks - 1);
-        const bool inside = kt.at(e) == at;
-        last_chunk = e - e0 >= n_st ? 2 * n_st - 1 : 2 * (e - e0) + (inside && (wave_hi & (KT - 1)) < 32 ? 0 : 1);
+        first_tile = 0;
+        while (first_tile < n_st && key_of(first_tile) > wave_hi) ++first_tile;
     }
 
-    auto step = [&](auto kb_tag, auto vb_tag, auto kc_tag, const f32x16& s_cur, f32x16& s_nxt, const bf16x8& pc0, const bf16x8& pc1, bf16x8& pn0,
-                    bf16x8& pn1, bf16x8 (&f)[4]) {
+    // key0: of the chunk whose products s_cur become weights
+    auto step = [&](auto kb_tag, auto vb_tag, auto kc_tag, int key0, const f32x16& s_cur, f32x16& s_nxt, const bf16x8& pc0, const bf16x8& pc1,
+                    bf16x8& pn0, bf16x8& pn1, bf16x8 (&f)[4]) __attribute__((always_inline)) {
         constexpr int KB = decltype(kb_tag)::value, VB = decltype(vb_tag)::value, KC = decltype(kc_tag)::value;
+        cw.at(m0, key0 + 8 * half - pos);
         const char* const vbase = ldsV + VB * TILE_B;
         auto operand = [&](auto j_tag) {            // operand j of this step (j < NG) or of the next one
             constexpr int J = decltype(j_tag)::value;
@@ -632,12 +715,12 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
             constexpr int g = decltype(g_tag)::value;
             group_mfma<g, D>(f[g % 4], qf, s_nxt, oacc, pc0, pc1);
             if constexpr (g + 3 < NG || KC == 0) f[(g + 3) % 4] = operand(IC<g + 3>{});
-            group_weights<g, D, true>(s_cur, c, mc, e, pn0, pn1, l_new);
+            group_mode_weights<g, D, MODE>(s_cur, cw, e, pn0, pn1, l_new);
             SPA_FENCE();
         };
         SPA_FENCE();
         static_for<NG>([&](auto g_tag) { group(g_tag); });
-        if (__any(!(l_new < limit))) raise(s_cur, pn0, pn1);
+        if (needs_mask(key0) || __any(!(l_new < limit))) slow_weights(s_cur, key0, pn0, pn1);
         else l = l_new;
     };
 
@@ -654,12 +737,11 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
         sB = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds16(ldsK + CHUNK_B + kofs[s]), qf[s], sB, 0, 0, 0);
     }
     bf16x8 pA0, pA1, pB0, pB1;                     // weights of even / odd chunks
-    finish(sA, key_of(0));
-    raise(sA, pA0, pA1);
+    slow_weights(sA, key_of(0), pA0, pA1);
 
     Pages pg2 = pages_of(2);
     // tile t = steps 2t and 2t + 1: reads K(t + 1) (logits ahead) and V^T(t)
-    auto one_tile = [&](auto par_tag, int t) {
+    auto one_tile = [&](auto par_tag, int t) __attribute__((always_inline)) {
         constexpr int PAR = decltype(par_tag)::value;      // t % 2
         using KB = IC<1 - PAR>;
         using VB = IC<PAR>;
@@ -676,20 +758,10 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
         if (t + 1 < n_st) issue_v(IC<1 - PAR>{}, t + 1, pg1);
         pg1 = pg2;
         pg2 = pages_of(t + 3);
-        const bool on = 2 * t <= last_chunk, on2 = 2 * t + 1 <= last_chunk;
-        if (on) {
-            finish(sB, key_of(t) + 32);
-            step(KB{}, VB{}, IC<0>{}, sB, sA, pA0, pA1, pB0, pB1, f);
-        }
-        if (on2) {
-            if (t + 1 >= n_st) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) sA[r] = -INFINITY;        // past the end: logits of a stale buffer
-            } else {
-                finish(sA, key_of(t + 1));
-            }
-            step(KB{}, VB{}, IC<1>{}, sA, sB, pB0, pB1, pA0, pA1, f);
-        }
+        if (t + 1 < first_tile) return;
+        step(KB{}, VB{}, IC<0>{}, key_of(t) + 32, sB, sA, pA0, pA1, pB0, pB1, f);
+        // past the end: products of a stale buffer, masked like keys behind every position
+        step(KB{}, VB{}, IC<1>{}, t + 1 < n_st ? key_of(t + 1) : 1 << 30, sA, sB, pB0, pB1, pA0, pA1, f);
     };
     for (int t = 0;;) {
         one_tile(IC<0>{}, t);
@@ -701,7 +773,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
     const float lt = l + other_half(l);
     const bool none = m == -INFINITY && lt == 0.f;         // a row that sees no key; NaN is not none
     const float inv = none ? 0.f : 1.f / lt;
-    const float lse2 = none ? -INFINITY : mc + __log2f(lt);
+    const float lse2 = none ? -INFINITY : m + __log2f(lt);
     if (!valid) return;
     if (partial) {
 #pragma unroll
@@ -848,15 +920,15 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
     if (parts.many.m) {
         const int64_t grid = most_units(d, parts.many);
         if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-        const bool mod = a.cap > 0.f || a.slopes != nullptr;
         const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, st, a, parts.many); };
-        if (a.log_p < 6) {
-            if (mod) go(paged_many_kernel<D, true, true>);
-            else go(paged_many_kernel<D, false, true>);
-        } else {
-            if (mod) go(paged_many_kernel<D, true, false>);
-            else go(paged_many_kernel<D, false, false>);
-        }
+        const auto with_pages = [&](auto mode) {
+            constexpr int MODE = decltype(mode)::value;
+            if (a.log_p < 6) go(paged_many_kernel<D, MODE, true>);
+            else go(paged_many_kernel<D, MODE, false>);
+        };
+        if (a.cap > 0.f) with_pages(IC<kCapped>{});
+        else if (a.slopes != nullptr) with_pages(IC<kSlopes>{});
+        else with_pages(IC<kPlain>{});
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -888,7 +960,7 @@ PagedParts paged_parts(const PagedDims& d, void* ws_or_null) {
         p.many.m = kManyRows;
         p.many.log_m = 7;
         p.many.span = (p.many.m + d.G - 1) / d.G + 1;
-        p.many.log_target = 9;
+        p.many.log_target = 10;
         p.many.min_tiles = 8;
         p.many.row_lo = p.few.m ? few_rows : 0;
         p.many.row_hi = 0x7fffffff;
