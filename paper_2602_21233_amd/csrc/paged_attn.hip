@@ -155,9 +155,11 @@ __device__ __forceinline__ float logit(const Logits& l, float s, int back) {
 __device__ __forceinline__ float max_over_groups(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
 __device__ __forceinline__ float sum_over_groups(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
 
-template <int D, int MF, bool MOD, bool SMALL>
-__global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs a, PagedPart part) {
-    constexpr int NW = 4;
+#ifndef AHEAD
+#define AHEAD 0
+#endif
+template <int D, int MF, bool MOD, bool SMALL, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, PagedPart part) {
     constexpr int DS = D / 32;        // MFMAs of a logits tile
     constexpr int DT = D / 16;        // 16-row tiles of O^T
     constexpr int PAD = D + 4;
@@ -205,29 +207,43 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs a, PagedPar
     const int32_t* const trow = a.table + (int64_t)sh.b * a.table_stride;
     auto page_of = [&](int key) { return clamp_int(trow[min(key >> a.log_p, last_col)], 0, a.n_pages - 1); };
     const int k_row = 8 * (n16 >> 2) + (n16 & 3);               // key of a chunk that this lane loads, and + 4
-
-    for (int c = 2 * cut * per + wave; c < 2 * e_end; c += NW) {
-        const int key0 = kt.at(c >> 1) * kPagedTile + 32 * (c & 1);
-        if (key0 > pos_hi) break;                               // only the last tile's second half
-        int id_k = page_of(key0), id_v = id_k;
-        if constexpr (SMALL) {                                  // pages of 16 tokens: a chunk lies in two
-            const int id1 = page_of(key0 + 16);
-            if (n16 >= 8) id_k = id1;
-            if (g >= 2) id_v = id1;
+    // chunks of this workgroup: the last tile's second half only if a row sees it
+    const int c_end = e_end == kt.n && (pos_hi & (kPagedTile - 1)) < 32 ? 2 * e_end - 1 : 2 * e_end;
+    auto key_of = [&](int c) { return kt.at(c >> 1) * kPagedTile + 32 * (c & 1); };
+    struct Pages {                                              // pages of 16 tokens: a chunk lies in two
+        int id[SMALL ? 2 : 1];
+    };
+    auto pages_of = [&](int c) {
+        Pages p;
+        const int key0 = key_of(min(c, c_end - 1));
+        p.id[0] = page_of(key0);
+        if constexpr (SMALL) p.id[1] = page_of(key0 + 16);
+        return p;
+    };
+    struct Chunk {
+        bf16x8 k0[DS], k1[DS];
+        u32x4 v[DT];
+    };
+    auto load = [&](int c, const Pages& pg, Chunk& ch) __attribute__((always_inline)) {
+        const int key0 = key_of(c);
+        int id_k = pg.id[0], id_v = pg.id[0];
+        if constexpr (SMALL) {
+            if (n16 >= 8) id_k = pg.id[1];
+            if (g >= 2) id_v = pg.id[1];
         }
         const int in_page = SMALL ? 0 : key0 & (page - 1);
         const uint16_t* kp = a.k + id_k * a.kp_p + kvh * a.kp_h + (in_page + (SMALL ? k_row & 15 : k_row)) * D + 8 * g;
         const uint16_t* vp = a.vt + id_v * a.vp_p + kvh * a.vp_h + in_page + 8 * (SMALL ? g & 1 : g) + (int64_t)n16 * page;
-        bf16x8 k0[DS], k1[DS];
-        u32x4 vv[DT];
 #pragma unroll
         for (int s = 0; s < DS; ++s) {
-            k0[s] = *reinterpret_cast<const bf16x8*>(kp + 32 * s);
-            k1[s] = *reinterpret_cast<const bf16x8*>(kp + 4 * D + 32 * s);
+            ch.k0[s] = *reinterpret_cast<const bf16x8*>(kp + 32 * s);
+            ch.k1[s] = *reinterpret_cast<const bf16x8*>(kp + 4 * D + 32 * s);
         }
 #pragma unroll
-        for (int t = 0; t < DT; ++t) vv[t] = *reinterpret_cast<const u32x4*>(vp + 16 * t * page);
-
+        for (int t = 0; t < DT; ++t) ch.v[t] = *reinterpret_cast<const u32x4*>(vp + 16 * t * page);
+    };
+    auto attend = [&](int c, Chunk& ch) __attribute__((always_inline)) {
+        const int key0 = key_of(c);
         // keys that no row of the tile sees: behind its last position, or between the sinks and its first window
         const int gone_lo = a.sink, gone_hi = a.window > 0 ? pos_lo - a.window + 1 : 0;       // [gone_lo, gone_hi)
         if (key0 + 31 > pos_hi || (key0 + 31 >= gone_lo && key0 < gone_hi)) {
@@ -240,7 +256,7 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs a, PagedPar
                           (kb <= pos_hi && !(kb >= gone_lo && kb < gone_hi) ? 0xffff0000u : 0u);
             }
 #pragma unroll
-            for (int t = 0; t < DT; ++t) vv[t] &= keep;
+            for (int t = 0; t < DT; ++t) ch.v[t] &= keep;
         }
         const bool masked = key0 + 31 > pos_lo || (a.window > 0 && key0 + 31 >= a.sink && key0 <= pos_hi - a.window);
 #pragma unroll
@@ -248,8 +264,8 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs a, PagedPar
             f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
 #pragma unroll
             for (int s = 0; s < DS; ++s) {
-                s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0[s], qf[f][s], s0, 0, 0, 0);
-                s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1[s], qf[f][s], s1, 0, 0, 0);
+                s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ch.k0[s], qf[f][s], s0, 0, 0, 0);
+                s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ch.k1[s], qf[f][s], s1, 0, 0, 0);
             }
             f32x8 x;
             const int back = pos[f] - key0 - 8 * g;
@@ -299,7 +315,42 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs a, PagedPar
             const bf16x8 p = __builtin_convertvector(w, bf16x8);
 #pragma unroll
             for (int t = 0; t < DT; ++t)
-                o[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vv[t]), p, o[f][t], 0, 0, 0);
+                o[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ch.v[t]), p, o[f][t], 0, 0, 0);
+        }
+    };
+    // The next chunk's loads fly while a chunk is computed, and its pages are looked up one chunk earlier still.  Two chunks of
+    // 32 rows with head_dim 128 do not fit the registers.
+    constexpr bool kAhead = D * MF <= AHEAD;
+    int c = 2 * cut * per + wave;
+    if (c < c_end) {
+        Pages pg = pages_of(c);
+        if constexpr (kAhead) {
+            Chunk one, two;
+            load(c, pg, one);
+            pg = pages_of(c + NW);
+            for (;; c += 2 * NW) {
+                if (c + NW >= c_end) {
+                    attend(c, one);
+                    break;
+                }
+                load(c + NW, pg, two);
+                pg = pages_of(c + 2 * NW);
+                attend(c, one);
+                if (c + 2 * NW >= c_end) {
+                    attend(c + NW, two);
+                    break;
+                }
+                load(c + 2 * NW, pg, one);
+                pg = pages_of(c + 3 * NW);
+                attend(c + NW, two);
+            }
+        } else {
+            for (; c < c_end; c += NW) {
+                Chunk one;
+                load(c, pg, one);
+                pg = pages_of(c + NW);
+                attend(c, one);
+            }
         }
     }
 
@@ -318,9 +369,9 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs a, PagedPar
 #pragma unroll
         for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(&s_o[wave][n16][16 * t + 4 * g]) = o[f][t];
         __syncthreads();
-        const int r16 = tid >> 4, d0 = (tid & 15) * (D / 16);    // 16 threads a row, D / 16 values each
+        const int r16 = (tid >> 4) & 15, d0 = (tid & 15) * (D / 16);   // 16 threads a row, D / 16 values each
         const int row = row0 + 16 * f + r16;
-        if (row <= last_row) {
+        if (tid < 256 && row <= last_row) {
             float mx = -INFINITY;
 #pragma unroll
             for (int w = 0; w < NW; ++w) mx = fmaxf(mx, s_m[w][16 * f + r16]);
@@ -894,16 +945,16 @@ int64_t most_slots(const PagedDims& d, const PagedPart& part) {
     return units < most ? units : most;
 }
 
-template <int D, int MF>
+template <int D, int MF, int NW>
 void launch_few(const PagedArgs& a, const PagedPart& part, unsigned grid, hipStream_t st) {
     const bool mod = a.cap > 0.f || a.slopes != nullptr;
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, a, part); };
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * NW), 0, st, a, part); };
     if (a.log_p == 4) {
-        if (mod) go(paged_few_kernel<D, MF, true, true>);
-        else go(paged_few_kernel<D, MF, false, true>);
+        if (mod) go(paged_few_kernel<D, MF, true, true, NW>);
+        else go(paged_few_kernel<D, MF, false, true, NW>);
     } else {
-        if (mod) go(paged_few_kernel<D, MF, true, false>);
-        else go(paged_few_kernel<D, MF, false, false>);
+        if (mod) go(paged_few_kernel<D, MF, true, false, NW>);
+        else go(paged_few_kernel<D, MF, false, false, NW>);
     }
 }
 
@@ -912,8 +963,9 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
     if (parts.few.m) {
         const int64_t grid = most_units(d, parts.few);
         if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-        if (parts.few.m == 16) launch_few<D, 1>(a, parts.few, (unsigned)grid, st);
-        else launch_few<D, 2>(a, parts.few, (unsigned)grid, st);
+        if (parts.few.m == 32) launch_few<D, 2, 4>(a, parts.few, (unsigned)grid, st);
+        else if (grid <= 256) launch_few<D, 1, 8>(a, parts.few, (unsigned)grid, st);
+        else launch_few<D, 1, 4>(a, parts.few, (unsigned)grid, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
