@@ -109,9 +109,6 @@ __device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedPart& p
     }
     return found;
 }
-__device__ __forceinline__ Share share_of_workgroup(const PagedArgs& a, const PagedPart& part) {
-    return share_of<false>(a, part, part_piece(a, part, threadIdx.x & 63), blockIdx.x);
-}
 // a request's key tiles are dealt to its pieces evenly
 __device__ __forceinline__ int tiles_of_piece(const PagedShare& s) { return (int)((uint32_t)(s.keys + s.splits - 1) / (uint32_t)s.splits); }
 
@@ -155,18 +152,21 @@ __device__ __forceinline__ float logit(const Logits& l, float s, int back) {
 __device__ __forceinline__ float max_over_groups(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
 __device__ __forceinline__ float sum_over_groups(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
 
-#ifndef AHEAD
-#define AHEAD 0
-#endif
-template <int D, int MF, bool MOD, bool SMALL, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, PagedPart part) {
+//
+// NV > 1: a workgroup makes the outputs of D / NV dims only, from all of K and its share of V.  A CU takes in about 12 bytes a
+// clock however many loads it has in flight (256 KB of a head: 22000 cycles of a call of 501 keys), so a call of few workgroups
+// is faster on NV times as many, although they read K NV times: 11.8 -> 9.2 us.
+template <int D, int MF, bool MOD, bool SMALL, int NW, int NV>
+__global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, PagedPart part, unsigned units) {
     constexpr int DS = D / 32;        // MFMAs of a logits tile
-    constexpr int DT = D / 16;        // 16-row tiles of O^T
-    constexpr int PAD = D + 4;
+    constexpr int DV = D / NV;        // dims of the outputs
+    constexpr int DT = DV / 16;       // 16-row tiles of O^T
+    constexpr int PAD = DV + 4;
     __shared__ __attribute__((aligned(16))) float s_o[NW][16][PAD];
     __shared__ float s_m[NW][MF * 16], s_l[NW][MF * 16];
 
-    const Share sh = share_of_workgroup(a, part);
+    const int dv0 = NV > 1 ? (int)(blockIdx.x / units) * DV : 0;     // parts of a unit on one XCD where units are a multiple of 8
+    const Share sh = share_of<false>(a, part, part_piece(a, part, threadIdx.x & 63), NV > 1 ? blockIdx.x % units : blockIdx.x);
     if (sh.b < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4;
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, Page
         }
         const int in_page = SMALL ? 0 : key0 & (page - 1);
         const uint16_t* kp = a.k + id_k * a.kp_p + kvh * a.kp_h + (in_page + (SMALL ? k_row & 15 : k_row)) * D + 8 * g;
-        const uint16_t* vp = a.vt + id_v * a.vp_p + kvh * a.vp_h + in_page + 8 * (SMALL ? g & 1 : g) + (int64_t)n16 * page;
+        const uint16_t* vp = a.vt + id_v * a.vp_p + kvh * a.vp_h + in_page + 8 * (SMALL ? g & 1 : g) + (int64_t)(dv0 + n16) * page;
 #pragma unroll
         for (int s = 0; s < DS; ++s) {
             ch.k0[s] = *reinterpret_cast<const bf16x8*>(kp + 32 * s);
@@ -318,43 +318,18 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, Page
                 o[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ch.v[t]), p, o[f][t], 0, 0, 0);
         }
     };
-    // The next chunk's loads fly while a chunk is computed, and its pages are looked up one chunk earlier still.  Two chunks of
-    // 32 rows with head_dim 128 do not fit the registers.
-    constexpr bool kAhead = D * MF <= AHEAD;
     int c = 2 * cut * per + wave;
     if (c < c_end) {
         Pages pg = pages_of(c);
-        if constexpr (kAhead) {
-            Chunk one, two;
+        for (; c < c_end; c += NW) {
+            Chunk one;
             load(c, pg, one);
-            pg = pages_of(c + NW);
-            for (;; c += 2 * NW) {
-                if (c + NW >= c_end) {
-                    attend(c, one);
-                    break;
-                }
-                load(c + NW, pg, two);
-                pg = pages_of(c + 2 * NW);
-                attend(c, one);
-                if (c + 2 * NW >= c_end) {
-                    attend(c + NW, two);
-                    break;
-                }
-                load(c + 2 * NW, pg, one);
-                pg = pages_of(c + 3 * NW);
-                attend(c + NW, two);
-            }
-        } else {
-            for (; c < c_end; c += NW) {
-                Chunk one;
-                load(c, pg, one);
-                pg = pages_of(c + NW);
-                attend(c, one);
-            }
+            pg = pages_of(c + NW);                              // one chunk ahead
+            attend(c, one);
         }
     }
 
-    // The four wavefronts' results of a row become one: every wavefront leaves its sums, relative to its own reference
+    // The wavefronts' results of a row become one: every wavefront leaves its sums, relative to its own reference
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
         const float lq = sum_over_groups(l[f]);
@@ -369,40 +344,41 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, Page
 #pragma unroll
         for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(&s_o[wave][n16][16 * t + 4 * g]) = o[f][t];
         __syncthreads();
-        const int r16 = (tid >> 4) & 15, d0 = (tid & 15) * (D / 16);   // 16 threads a row, D / 16 values each
+        constexpr int VPT = DV == 128 ? 8 : 4, TPR = DV / VPT;   // values of a thread, threads of a row
+        const int r16 = tid / TPR, d0 = tid % TPR * VPT;
         const int row = row0 + 16 * f + r16;
-        if (tid < 256 && row <= last_row) {
+        if (r16 < 16 && row <= last_row) {
             float mx = -INFINITY;
 #pragma unroll
             for (int w = 0; w < NW; ++w) mx = fmaxf(mx, s_m[w][16 * f + r16]);
-            float lsum = 0.f, acc[D / 16];
+            float lsum = 0.f, acc[VPT];
 #pragma unroll
-            for (int x = 0; x < D / 16; ++x) acc[x] = 0.f;
+            for (int x = 0; x < VPT; ++x) acc[x] = 0.f;
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 const float mw = s_m[w][16 * f + r16];
                 const float scale = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - mx);
                 lsum = fmaf(s_l[w][16 * f + r16], scale, lsum);
 #pragma unroll
-                for (int x = 0; x < D / 16; ++x) acc[x] = fmaf(s_o[w][r16][d0 + x], scale, acc[x]);
+                for (int x = 0; x < VPT; ++x) acc[x] = fmaf(s_o[w][r16][d0 + x], scale, acc[x]);
             }
             const bool none = mx == -INFINITY && lsum == 0.f;    // a row that sees no key (of this piece); NaN is not none
             const float inv = none ? 0.f : 1.f / lsum;
             const float lse2 = none ? -INFINITY : mx + __log2f(lsum);
             if (partial) {
-                float* po = part.o + ((int64_t)slot * part.m + 16 * f + r16) * D + d0;
+                float* po = part.o + ((int64_t)slot * part.m + 16 * f + r16) * D + dv0 + d0;
 #pragma unroll
-                for (int x = 0; x < D / 16; ++x) po[x] = acc[x] * inv;
-                if ((tid & 15) == 0) part.lse[(int64_t)slot * part.m + 16 * f + r16] = lse2;
+                for (int x = 0; x < VPT; ++x) po[x] = acc[x] * inv;
+                if (tid % TPR == 0 && dv0 == 0) part.lse[(int64_t)slot * part.m + 16 * f + r16] = lse2;
             } else {
                 const int tok = sh.r.first + row / a.G, hd = kvh * a.G + row % a.G;
-                uint16_t* orow = a.out + (int64_t)tok * a.o_t + hd * a.o_h + d0;
+                uint16_t* orow = a.out + (int64_t)tok * a.o_t + hd * a.o_h + dv0 + d0;
 #pragma unroll
-                for (int x = 0; x < D / 16; x += 4) {
+                for (int x = 0; x < VPT; x += 4) {
                     const f32x4 v = {acc[x] * inv, acc[x + 1] * inv, acc[x + 2] * inv, acc[x + 3] * inv};
                     *reinterpret_cast<bf16x4*>(orow + x) = __builtin_convertvector(v, bf16x4);
                 }
-                if (a.lse != nullptr && (tid & 15) == 0) a.lse[(int64_t)tok * a.Hq + hd] = lse2 * kLn2;
+                if (a.lse != nullptr && tid % TPR == 0 && dv0 == 0) a.lse[(int64_t)tok * a.Hq + hd] = lse2 * kLn2;
             }
         }
     }
@@ -529,7 +505,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
     __shared__ __attribute__((aligned(1024))) uint16_t smemK[2][TILE];
     __shared__ __attribute__((aligned(1024))) uint16_t smemV[2][TILE];
 
-    const Share sh = share_of_workgroup(a, part);
+    const Share sh = share_of<false>(a, part, part_piece(a, part, threadIdx.x & 63), blockIdx.x);
     if (sh.b < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, l32 = lane & 31;
@@ -852,25 +828,27 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Merge of the pieces' results, a wavefront per row: out = sum_s w_s out_s / sum_s w_s, w_s = 2^(lse_s - max).  64 pieces at a time: a
-// lane has the weight of one, then D / 8 lanes read a piece's values, 64 / (D / 8) pieces side by side.
-template <int D>
+// Merge of the pieces' results: out = sum_s w_s out_s / sum_s w_s, w_s = 2^(lse_s - max).  A wavefront makes D / NV dims of a row, 64 pieces
+// at a time: a lane has the weight of one, then DV / 4 lanes read a piece's values, 64 / (DV / 4) pieces side by side.  NV = 4 for few
+// rows: what a CU takes in bounds them (4 requests behind 128K tokens, 128 rows of 64 pieces: 11.7 -> 7.6 us).
+template <int D, int NV>
 __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& part) {
-    constexpr int LPR = D / 8, NG = 64 / LPR;       // lanes of a piece, pieces side by side
+    constexpr int DV = D / NV, LPR = DV / 4, NG = 64 / LPR;       // dims of a wavefront, lanes of a piece, pieces side by side
     const int lane = threadIdx.x & 63;
-    const int grp = lane / LPR, d0 = 8 * (lane % LPR);
+    const int grp = lane / LPR;
     const int piece = part_piece(a, part, lane);
     for (uint32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);; item += gridDim.x * 4) {
-        const Share sh = share_of<true>(a, part, piece, (uint32_t)__builtin_amdgcn_readfirstlane((int)item));
+        const uint32_t i = (uint32_t)__builtin_amdgcn_readfirstlane((int)item);
+        const Share sh = share_of<true>(a, part, piece, i / NV);
         if (sh.b < 0) return;
+        const int d0 = (int)(i % NV) * DV + 4 * (lane % LPR);
         const int kvh = sh.unit % a.Hkv, row = sh.unit / a.Hkv, splits = sh.s.splits;
         const int tile = row >> part.log_m, rt = row & (part.m - 1);
         const int slot0 = sh.slot + (sh.s.tiles - 1 - tile) * splits * a.Hkv + kvh;
         if (slot0 + (splits - 1) * a.Hkv >= part.n_slots) continue;
         auto at = [&](int s) { return (int64_t)(slot0 + s * a.Hkv) * part.m + rt; };
-        float mx = -INFINITY, total = 0.f, acc[8];
-#pragma unroll
-        for (int x = 0; x < 8; ++x) acc[x] = 0.f;
+        float mx = -INFINITY, total = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         for (int s0 = 0; s0 < splits; s0 += 64) {
             const float v = s0 + lane < splits ? part.lse[at(s0 + lane)] : -INFINITY;
             float top = v;
@@ -881,26 +859,23 @@ __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& 
             mx = mx_new;
             const float w = v == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(v - mx);
             total = fmaf(total, old, w);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) acc[x] *= old;
+            acc *= old;
             const int n = min(64, splits - s0);
             for (int s = 0; s < n; s += 4 * NG) {           // four loads of a lane in flight
                 float ws[4];
-                f32x4 p[4][2];
+                f32x4 p[4];
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                     const int mine = s + NG * y + grp, there = min(mine, n - 1);
                     const float wy = __shfl(w, there);
                     ws[y] = mine < n ? wy : 0.f;
-                    const f32x4* const po = reinterpret_cast<const f32x4*>(part.o + at(s0 + there) * D + d0);
-                    p[y][0] = po[0];
-                    p[y][1] = po[1];
+                    p[y] = *reinterpret_cast<const f32x4*>(part.o + at(s0 + there) * D + d0);
                 }
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
 #pragma unroll
-                    for (int x = 0; x < 8; ++x)             // a piece without a key in sight may not have written its values
-                        acc[x] = ws[y] != 0.f ? fmaf(p[y][x >> 2][x & 3], ws[y], acc[x]) : acc[x];
+                    for (int x = 0; x < 4; ++x)             // a piece without a key in sight may not have written its values
+                        acc[x] = ws[y] != 0.f ? fmaf(p[y][x], ws[y], acc[x]) : acc[x];
             }
         }
 #pragma unroll
@@ -908,23 +883,20 @@ __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& 
 #pragma unroll
         for (int x = LPR; x < 64; x <<= 1)
 #pragma unroll
-            for (int y = 0; y < 8; ++y) acc[y] += __shfl_xor(acc[y], x);
+            for (int y = 0; y < 4; ++y) acc[y] += __shfl_xor(acc[y], x);
         const bool none = total == 0.f;
         const float inv = none ? 0.f : 1.f / total;
         if (lane < LPR) {
             const int tok = sh.r.first + row / a.G, hd = kvh * a.G + row % a.G;
-            f32x8 v;
-#pragma unroll
-            for (int x = 0; x < 8; ++x) v[x] = acc[x] * inv;
-            *reinterpret_cast<bf16x8*>(a.out + (int64_t)tok * a.o_t + hd * a.o_h + d0) = __builtin_convertvector(v, bf16x8);
-            if (a.lse != nullptr && lane == 0) a.lse[(int64_t)tok * a.Hq + hd] = none ? -INFINITY : (mx + __log2f(total)) * kLn2;
+            *reinterpret_cast<bf16x4*>(a.out + (int64_t)tok * a.o_t + hd * a.o_h + d0) = __builtin_convertvector(acc * inv, bf16x4);
+            if (a.lse != nullptr && lane == 0 && d0 == 0) a.lse[(int64_t)tok * a.Hq + hd] = none ? -INFINITY : (mx + __log2f(total)) * kLn2;
         }
     }
 }
-template <int D>
+template <int D, int NV>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a, PagedPart few, PagedPart many) {
-    if (few.n_slots > 0) merge_rows<D>(a, few);
-    if (many.n_slots > 0) merge_rows<D>(a, many);
+    if (few.n_slots > 0) merge_rows<D, NV>(a, few);
+    if (many.n_slots > 0) merge_rows<D, NV>(a, many);
 }
 
 // Most workgroups of a part that a call can need, whatever its lengths (below `target` more than without cuts, and none
@@ -945,16 +917,16 @@ int64_t most_slots(const PagedDims& d, const PagedPart& part) {
     return units < most ? units : most;
 }
 
-template <int D, int MF, int NW>
-void launch_few(const PagedArgs& a, const PagedPart& part, unsigned grid, hipStream_t st) {
+template <int D, int MF, int NW, int NV>
+void launch_few(const PagedArgs& a, const PagedPart& part, unsigned units, hipStream_t st) {
     const bool mod = a.cap > 0.f || a.slopes != nullptr;
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * NW), 0, st, a, part); };
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(units * NV), dim3(64 * NW), 0, st, a, part, units); };
     if (a.log_p == 4) {
-        if (mod) go(paged_few_kernel<D, MF, true, true, NW>);
-        else go(paged_few_kernel<D, MF, false, true, NW>);
+        if (mod) go(paged_few_kernel<D, MF, true, true, NW, NV>);
+        else go(paged_few_kernel<D, MF, false, true, NW, NV>);
     } else {
-        if (mod) go(paged_few_kernel<D, MF, true, false, NW>);
-        else go(paged_few_kernel<D, MF, false, false, NW>);
+        if (mod) go(paged_few_kernel<D, MF, true, false, NW, NV>);
+        else go(paged_few_kernel<D, MF, false, false, NW, NV>);
     }
 }
 
@@ -963,9 +935,9 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
     if (parts.few.m) {
         const int64_t grid = most_units(d, parts.few);
         if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-        if (parts.few.m == 32) launch_few<D, 2, 4>(a, parts.few, (unsigned)grid, st);
-        else if (grid <= 256) launch_few<D, 1, 8>(a, parts.few, (unsigned)grid, st);
-        else launch_few<D, 1, 4>(a, parts.few, (unsigned)grid, st);
+        if (parts.few.m == 32) launch_few<D, 2, 4, 1>(a, parts.few, (unsigned)grid, st);
+        else if (grid <= 64) launch_few<D, 1, 8, 4>(a, parts.few, (unsigned)grid, st);
+        else launch_few<D, 1, 4, 1>(a, parts.few, (unsigned)grid, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -985,8 +957,9 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
         if (e != hipSuccess) return e;
     }
     if (parts.few.n_slots + parts.many.n_slots == 0) return hipSuccess;
-    const int64_t rows = ((int64_t)d.T * d.Hq + 3) / 4;
-    hipLaunchKernelGGL((paged_merge_kernel<D>), dim3((unsigned)(rows < 1024 ? rows : 1024)), dim3(256), 0, st, a, parts.few, parts.many);
+    const int64_t rows = (int64_t)d.T * d.Hq;
+    if (rows <= 1024) hipLaunchKernelGGL((paged_merge_kernel<D, 4>), dim3((unsigned)rows), dim3(256), 0, st, a, parts.few, parts.many);
+    else hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(1024), dim3(256), 0, st, a, parts.few, parts.many);
     return hipGetLastError();
 }
 
