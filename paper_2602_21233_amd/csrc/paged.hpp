@@ -18,13 +18,15 @@ struct PagedDims {
 
 // One of the two attention kernels.  It serves the requests with row_lo < rows <= row_hi, rows = new tokens * query heads of a
 // KV head, m = 2^log_m rows a workgroup (0: no such kernel in the call), which span at most `span` tokens, and cuts the key axis
-// so that about 2^log_target workgroups come about, each of at least `min_tiles` key tiles.
+// into pieces: of at least `min_tiles` key tiles, and so that at most 2^log_most of them come about beyond one for every row tile.
 struct PagedPart {
     int m, log_m, span;
-    int log_target, min_tiles;
+    int log_most, min_tiles;
+    int whole_tiles;                  // tables of up to so many key tiles are not cut at all (no workspace, no merge)
     int row_lo, row_hi;
-    int n_slots;                      // partial results that the workspace has room for
+    int n_slots;                      // partial results that the workspace has room for; 0: nothing is cut
     float *o, *lse;                   // partial results: [n_slots][m][D], [n_slots][m]; lse in base 2
+    int32_t* piece;                   // many rows: key tiles of a piece, as the attention kernel leaves them for the merge
 };
 
 // A request's share of a part: row tiles, key tiles (of its longest row tile), pieces of the key axis
@@ -61,10 +63,22 @@ __host__ __device__ __forceinline__ int most_key_tiles(int q_len, int kv_len, in
     return some < all ? (int)some : all;
 }
 
-// key tiles of a piece of the key axis, for `work` (row tile, key tile, KV head) triples in all; a key axis has at most 2^24
-__host__ __device__ __forceinline__ int piece_of(int64_t work, const PagedPart& part) {
-    const int64_t even = (work + (1ll << part.log_target) - 1) >> part.log_target;
-    return even < part.min_tiles ? part.min_tiles : (even > (1 << 24) ? 1 << 24 : (int)even);
+constexpr int kWholeAxis = 1 << 24;   // key tiles: more than any key axis has
+__host__ __device__ __forceinline__ int piece_within(int64_t tiles, const PagedPart& part) {
+    return tiles < part.min_tiles ? part.min_tiles : (tiles > kWholeAxis ? kWholeAxis : (int)tiles);
+}
+// Key tiles of a piece, for `work` (row tile, key tile, KV head) triples in all.
+// The shortest that the workspace has room for:
+__host__ __device__ __forceinline__ int shortest_piece(int64_t work, const PagedPart& part) {
+    return piece_within((work + (1ll << part.log_most) - 1) >> part.log_most, part);
+}
+// The kernel for few rows: short enough for 512 workgroups, then not below 16 tiles (a workgroup that starts costs about as much as
+// two tiles) until these are more than the workspace's.  Measured with 2^11 = log_most always, or 16 tiles at least: 32 requests with a window of
+// 4096 tokens 61.9 / 59.4 us, drafted tokens of 32 requests 65.9 / 64.6, 16 requests of 2400 tokens 24.0 with 4 tiles / 27.4.
+__host__ __device__ __forceinline__ int few_rows_piece(int64_t work, const PagedPart& part) {
+    const int64_t even = (work + 511) >> 9;
+    const int p = piece_within(even < 16 ? even : 16, part), least = shortest_piece(work, part);
+    return p > least ? p : least;
 }
 __host__ __device__ __forceinline__ PagedShare paged_share(const PagedPart& part, int G, int q_len, int kv_len, int sink, int window, int piece) {
     PagedShare s{0, 0, 0};

@@ -58,17 +58,66 @@ __device__ __forceinline__ Request request_at(const PagedArgs& a, int b) {
 __device__ __forceinline__ PagedShare share_at(const PagedArgs& a, const PagedPart& part, const Request& r, int piece) {
     return paged_share(part, a.G, r.len, r.kv, a.sink, a.window, piece);
 }
+// sum and maximum over the 16 lanes of a row, in its last lane
+__device__ __forceinline__ uint32_t row_sum(uint32_t v) {
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, true);
+    return v;
+}
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, true));
+    return v;
+}
+// The kernel for many rows, up to 64 requests: of four lengths of a piece the one with the least time, by a model.  512 workgroups run
+// at once and take about 1.6 us a key tile: the longest piece, or the rounds of average ones, whichever is more; then the merge, 5 us and
+// 0.03 for each piece.  With 2^9 pieces always, or 2^10: chunk of 2048 tokens 3040 / 3105 us, mixed step 493 / 455.  Short calls want
+// more pieces (87 tokens over 800, 12 row tiles of 14 tiles: in pieces of 7 tiles 27 us, of 2 19), those whose row tiles fill the chip none.
+// A row of 16 lanes tries one length.
+__device__ __forceinline__ int many_rows_piece(const PagedArgs& a, const PagedPart& part, int64_t work, int lane) {
+    const int least = shortest_piece(work, part);
+    const int base = piece_within((work + 511) >> 9, part);
+    const int turn = lane >> 4;
+    int p = turn == 0 ? kWholeAxis : base < 8 ? base << (turn - 1) : turn == 1 ? base >> 1 : turn == 2 ? base : 2 * base;
+    if (p < least) p = least;
+    uint32_t units = 0, cut = 0, longest = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 16) {
+        const PagedShare s = share_at(a, part, request_at(a, b0 + (lane & 15)), p);
+        const uint32_t mine = (uint32_t)(s.tiles * s.splits) * (uint32_t)a.Hkv;
+        units += mine;
+        cut += s.splits > 1 ? mine : 0u;
+        longest = max(longest, (uint32_t)min(s.keys, p));
+    }
+    units = row_sum(units);
+    cut = row_sum(cut);
+    const float rounds = ceilf((float)units * (1.f / 512.f)) * (float)work / (float)max(units, 1u);
+    const float us = 1.6f * fmaxf((float)row_max(longest), rounds) + (cut > 0 ? 5.f + 0.03f * (float)cut : 0.f);
+    auto time_of = [&](int t) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane(__float_as_int(us), 16 * t + 15)); };
+    int best = 0;
+#pragma unroll
+    for (int t = 1; t < 4; ++t)
+        if (time_of(t) < time_of(best)) best = t;
+    return __builtin_amdgcn_readlane(p, 16 * best + 15);
+}
 // key tiles of a part's pieces, the same in every lane
-__device__ __forceinline__ int part_piece(const PagedArgs& a, const PagedPart& part, int lane) {
+template <bool MANY>
+__device__ __forceinline__ int part_piece(const PagedArgs& a, const PagedPart& part, const Request& first, int lane) {
+    if (part.n_slots == 0) return kWholeAxis;
     int64_t work = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const PagedShare s = share_at(a, part, request_at(a, b0 + lane), 1 << 24);
+        const PagedShare s = share_at(a, part, b0 == 0 ? first : request_at(a, b0 + lane), kWholeAxis);
         work += (int64_t)s.tiles * s.keys;
     }
     // the lanes' sum in two halves of 24 bits; a lane's work of 2^48 and more makes the piece as long as any key axis either way
     const uint32_t lo = last_lane(wave_scan((uint32_t)(work & 0xffffff)));
     const uint32_t hi = last_lane(wave_scan((uint32_t)(work >> 24 > 0xffffff ? 0xffffff : work >> 24)));
-    return piece_of((((int64_t)hi << 24) + lo) * a.Hkv, part);
+    work = (((int64_t)hi << 24) + lo) * a.Hkv;
+    if constexpr (!MANY) return few_rows_piece(work, part);
+    else return a.B <= 64 ? many_rows_piece(a, part, work, lane) : shortest_piece(work, part);
 }
 
 // What a workgroup of a part serves: unit `unit` of request b, counted from the longest row tiles, KV heads next to each
@@ -80,14 +129,15 @@ struct Share {
     Request r;
 };
 // MERGE: units are the rows of requests whose keys are cut, KV heads next to each other
+// first: request_at(a, lane), which a caller has at hand or has in flight together with other loads
 template <bool MERGE>
-__device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedPart& part, int piece, uint32_t item) {
+__device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedPart& part, int piece, const Request& first, uint32_t item) {
     const int lane = threadIdx.x & 63;
     uint32_t items_before = 0, slots_before = 0;
     Share found;
     found.b = -1;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const Request r = request_at(a, b0 + lane);
+        const Request r = b0 == 0 ? first : request_at(a, b0 + lane);
         const PagedShare s = share_at(a, part, r, piece);
         const uint32_t units = (uint32_t)s.tiles * (uint32_t)s.splits * (uint32_t)a.Hkv;
         const uint32_t slots = s.splits > 1 ? units : 0u;
@@ -166,7 +216,9 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, Page
     __shared__ float s_m[NW][MF * 16], s_l[NW][MF * 16];
 
     const int dv0 = NV > 1 ? (int)(blockIdx.x / units) * DV : 0;     // parts of a unit on one XCD where units are a multiple of 8
-    const Share sh = share_of<false>(a, part, part_piece(a, part, threadIdx.x & 63), NV > 1 ? blockIdx.x % units : blockIdx.x);
+    const Request first = request_at(a, threadIdx.x & 63);
+    const int piece = part_piece<false>(a, part, first, threadIdx.x & 63);
+    const Share sh = share_of<false>(a, part, piece, first, NV > 1 ? blockIdx.x % units : blockIdx.x);
     if (sh.b < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4;
@@ -393,28 +445,29 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, Page
 // logits first and its reference hardly moves.
 constexpr int kManyRows = 128;
 
-enum Mode { kPlain, kSlopes, kCapped };        // scaled products; with a bias by distance; capped (and maybe biased)
+enum Mode { kPlain, kSlopes, kCapped, kCappedSlopes };   // scaled products; with a bias by distance; capped; both
 
 // What the running softmax of a wavefront needs of its row for a chunk: the weight of the product s in register r (key key0 +
 // 16 (r / 8) + 8 half + r % 8) is 2^(s c + bias(r)), or with a cap 2^(bias(r) - 2 cap2 / (1 + 2^(s k))), the same as
 // cap2 tanh(...) since tanh y = 1 - 2 / (1 + e^2y).  bias holds - m, the cap and the slope's share.
 template <int MODE>
 struct ChunkWeights {
+    static constexpr bool kCap = MODE == kCapped || MODE == kCappedSlopes, kBias = MODE == kSlopes || MODE == kCappedSlopes;
     float c, k, cap2, slope2, base;
     static __device__ __forceinline__ constexpr int key_of(int r) { return 16 * (r >> 3) + (r & 7); }
     // ahead: position of register 0's key less the row's own.  The biases are counted from the lane's last key (r = 15): for keys
     // that all lie at or before the row the two parts have one sign, so no precision is lost where a bias is small.
     __device__ __forceinline__ void at(float m, int ahead) {
-        const float less_m = MODE == kCapped ? cap2 - m : -m;
-        base = MODE == kPlain ? less_m : fmaf(slope2, (float)(ahead + key_of(15)), less_m);
+        const float less_m = kCap ? cap2 - m : -m;
+        base = kBias ? fmaf(slope2, (float)(ahead + key_of(15)), less_m) : less_m;
     }
-    __device__ __forceinline__ float bias(int r) const { return MODE == kPlain ? base : fmaf(slope2, (float)(key_of(r) - key_of(15)), base); }
+    __device__ __forceinline__ float bias(int r) const { return kBias ? fmaf(slope2, (float)(key_of(r) - key_of(15)), base) : base; }
     __device__ __forceinline__ float growth(float s) const { return __builtin_amdgcn_exp2f(s * k); }
     // the exponent as a masked chunk needs it, where keys lie on both sides of the row
     __device__ __forceinline__ float exponent(float s, int r, float m, int ahead) const {
-        const float less_m = MODE == kCapped ? cap2 - m : -m;
-        const float b = MODE == kPlain ? less_m : fmaf(slope2, (float)(ahead + key_of(r)), less_m);
-        if constexpr (MODE == kCapped) return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + growth(s)), b);
+        const float less_m = kCap ? cap2 - m : -m;
+        const float b = kBias ? fmaf(slope2, (float)(ahead + key_of(r)), less_m) : less_m;
+        if constexpr (kCap) return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + growth(s)), b);
         else return fmaf(s, c, b);
     }
 };
@@ -425,7 +478,7 @@ template <int g, int D, int MODE>
 __device__ __forceinline__ void group_mode_weights(const f32x16& s, const ChunkWeights<MODE>& cw, f32x8& e, bf16x8& pn0, bf16x8& pn1, float& l_new) {
     constexpr int NG = D / 8, HG = NG / 2;
     constexpr int hb = (g / HG) * 8, gg = g % HG;
-    constexpr bool first_half = g < HG;
+    constexpr bool first_half = g < HG, kCap = ChunkWeights<MODE>::kCap;
     auto linear = [&](int x0, int n) {
 #pragma unroll
         for (int x = x0; x < x0 + n; ++x) e[x] = fmaf(s[hb + x], cw.c, cw.bias(hb + x));
@@ -453,7 +506,7 @@ __device__ __forceinline__ void group_mode_weights(const f32x16& s, const ChunkW
         else pn1 = __builtin_convertvector(e, bf16x8);
         if constexpr (g == NG - 1) asm volatile("" : "+v"(l_new));   // keep the sums inside their groups
     };
-    if constexpr (HG == 8 && MODE != kCapped) {
+    if constexpr (HG == 8 && !kCap) {
         if constexpr (gg < 2) linear(4 * gg, 4);
         else if constexpr (gg < 6) exps(2 * (gg - 2), 2);
         else if constexpr (gg == 7) finish();
@@ -464,7 +517,7 @@ __device__ __forceinline__ void group_mode_weights(const f32x16& s, const ChunkW
         else if constexpr (gg == 5) exps(1, 4);
         else if constexpr (gg == 6) exps(5, 3);
         else finish();
-    } else if constexpr (MODE != kCapped) {
+    } else if constexpr (!kCap) {
         if constexpr (gg == 0) linear(0, 8);
         else if constexpr (gg < 3) exps(4 * (gg - 1), 4);
         else finish();
@@ -505,7 +558,10 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
     __shared__ __attribute__((aligned(1024))) uint16_t smemK[2][TILE];
     __shared__ __attribute__((aligned(1024))) uint16_t smemV[2][TILE];
 
-    const Share sh = share_of<false>(a, part, part_piece(a, part, threadIdx.x & 63), blockIdx.x);
+    const Request first = request_at(a, threadIdx.x & 63);
+    const int piece = part_piece<true>(a, part, first, threadIdx.x & 63);
+    if (part.n_slots > 0 && blockIdx.x == 0 && threadIdx.x == 0) *part.piece = piece;
+    const Share sh = share_of<false>(a, part, piece, first, blockIdx.x);
     if (sh.b < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, l32 = lane & 31;
@@ -662,8 +718,8 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
     ChunkWeights<MODE> cw;
     cw.c = a.scale * kLog2e;
     cw.cap2 = a.cap * kLog2e;
-    cw.k = MODE == kCapped ? 2.f * cw.c / a.cap : 0.f;
-    cw.slope2 = MODE != kPlain && a.slopes != nullptr ? a.slopes[head] * kLog2e : 0.f;
+    cw.k = ChunkWeights<MODE>::kCap ? 2.f * cw.c / a.cap : 0.f;
+    cw.slope2 = ChunkWeights<MODE>::kBias ? a.slopes[head] * kLog2e : 0.f;
     float m = -INFINITY, m0 = 0.f, l = 0.f, limit = -1.f;                     // m0: m, or 0 where that is -inf
     const int wave_row = row0 + 32 * wave;                                    // wave-uniform bounds of this wavefront's rows
     const int wave_lo = pos0 + min(wave_row, last_row) / a.G, wave_hi = pos0 + min(wave_row + 31, last_row) / a.G;
@@ -831,15 +887,17 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
 // Merge of the pieces' results: out = sum_s w_s out_s / sum_s w_s, w_s = 2^(lse_s - max).  A wavefront makes D / NV dims of a row, 64 pieces
 // at a time: a lane has the weight of one, then DV / 4 lanes read a piece's values, 64 / (DV / 4) pieces side by side.  NV = 4 for few
 // rows: what a CU takes in bounds them (4 requests behind 128K tokens, 128 rows of 64 pieces: 11.7 -> 7.6 us).
-template <int D, int NV>
+template <int D, int NV, bool MANY>
 __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& part) {
     constexpr int DV = D / NV, LPR = DV / 4, NG = 64 / LPR;       // dims of a wavefront, lanes of a piece, pieces side by side
     const int lane = threadIdx.x & 63;
     const int grp = lane / LPR;
-    const int piece = part_piece(a, part, lane);
+    const Request first = request_at(a, lane);
+    // found anew, or, where that takes longer than a load, as the attention kernel has left it
+    const int piece = MANY ? __builtin_amdgcn_readfirstlane(*part.piece) : part_piece<false>(a, part, first, lane);
     for (uint32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);; item += gridDim.x * 4) {
         const uint32_t i = (uint32_t)__builtin_amdgcn_readfirstlane((int)item);
-        const Share sh = share_of<true>(a, part, piece, i / NV);
+        const Share sh = share_of<true>(a, part, piece, first, i / NV);
         if (sh.b < 0) return;
         const int d0 = (int)(i % NV) * DV + 4 * (lane % LPR);
         const int kvh = sh.unit % a.Hkv, row = sh.unit / a.Hkv, splits = sh.s.splits;
@@ -895,25 +953,24 @@ __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& 
 }
 template <int D, int NV>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a, PagedPart few, PagedPart many) {
-    if (few.n_slots > 0) merge_rows<D, NV>(a, few);
-    if (many.n_slots > 0) merge_rows<D, NV>(a, many);
+    if (few.n_slots > 0) merge_rows<D, NV, false>(a, few);
+    if (many.n_slots > 0) merge_rows<D, NV, true>(a, many);
 }
 
-// Most workgroups of a part that a call can need, whatever its lengths (below `target` more than without cuts, and none
-// cut into pieces of less than min_tiles)
+// Most workgroups of a part that a call can need, whatever its lengths (2^log_most more than without cuts, and none cut into pieces
+// of less than min_tiles)
+int64_t key_tiles_of_table(const PagedDims& d) { return (((int64_t)d.C << d.log_p) + kPagedTile - 1) / kPagedTile; }
 int64_t most_units(const PagedDims& d, const PagedPart& part) {
     const int64_t requests = d.B < d.T ? d.B : d.T;
     const int64_t tiles = (part.row_hi <= part.m ? requests : (int64_t)d.T * d.G / part.m + requests) * d.Hkv;
-    const int64_t keys = (((int64_t)d.C << d.log_p) + kPagedTile - 1) / kPagedTile;
-    const int64_t cuts = (keys + part.min_tiles - 1) / part.min_tiles;
-    const int64_t target = 1ll << part.log_target;
-    return cuts <= 1 || tiles * cuts < tiles + target ? tiles * (cuts > 1 ? cuts : 1) : tiles + target;
+    if (key_tiles_of_table(d) <= part.whole_tiles) return tiles;
+    const int64_t most = 1ll << part.log_most, cuts = (key_tiles_of_table(d) + part.min_tiles - 1) / part.min_tiles;
+    return tiles * cuts < tiles + most ? tiles * cuts : tiles + most;
 }
 // Most partial results: requests that are cut have at most twice as many pieces as their work fills
 int64_t most_slots(const PagedDims& d, const PagedPart& part) {
-    const int64_t keys = (((int64_t)d.C << d.log_p) + kPagedTile - 1) / kPagedTile;
-    if (keys <= part.min_tiles) return 0;
-    const int64_t units = most_units(d, part), most = 2ll << part.log_target;
+    if (key_tiles_of_table(d) <= part.whole_tiles) return 0;
+    const int64_t units = most_units(d, part), most = 2ll << part.log_most;
     return units < most ? units : most;
 }
 
@@ -950,7 +1007,8 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
             if (a.log_p < 6) go(paged_many_kernel<D, MODE, true>);
             else go(paged_many_kernel<D, MODE, false>);
         };
-        if (a.cap > 0.f) with_pages(IC<kCapped>{});
+        if (a.cap > 0.f && a.slopes != nullptr) with_pages(IC<kCappedSlopes>{});
+        else if (a.cap > 0.f) with_pages(IC<kCapped>{});
         else if (a.slopes != nullptr) with_pages(IC<kSlopes>{});
         else with_pages(IC<kPlain>{});
         const hipError_t e = hipGetLastError();
@@ -976,8 +1034,9 @@ PagedParts paged_parts(const PagedDims& d, void* ws_or_null) {
         p.few.m = few_rows;
         p.few.log_m = few_rows == 16 ? 4 : 5;
         p.few.span = (p.few.m + d.G - 1) / d.G + 1;
-        p.few.log_target = 11;
-        p.few.min_tiles = 8;
+        p.few.log_most = 11;
+        p.few.min_tiles = 4;
+        p.few.whole_tiles = 8;
         p.few.row_lo = 0;
         p.few.row_hi = most_rows <= few_rows ? 0x7fffffff : few_rows;
     }
@@ -985,8 +1044,9 @@ PagedParts paged_parts(const PagedDims& d, void* ws_or_null) {
         p.many.m = kManyRows;
         p.many.log_m = 7;
         p.many.span = (p.many.m + d.G - 1) / d.G + 1;
-        p.many.log_target = 10;
-        p.many.min_tiles = 8;
+        p.many.log_most = 10;
+        p.many.min_tiles = 2;
+        p.many.whole_tiles = 8;
         p.many.row_lo = p.few.m ? few_rows : 0;
         p.many.row_hi = 0x7fffffff;
     }
@@ -999,6 +1059,8 @@ PagedParts paged_parts(const PagedDims& d, void* ws_or_null) {
         off += (size_t)part->n_slots * part->m * d.D * sizeof(float);
         part->lse = (float*)(base + off);
         off += ((size_t)part->n_slots * part->m * sizeof(float) + 255) / 256 * 256;
+        part->piece = (int32_t*)(base + off);
+        if (part->n_slots > 0 && part == &p.many) off += 256;
     }
     p.ws_bytes = off;
     return p;

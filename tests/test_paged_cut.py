@@ -10,7 +10,7 @@ SOURCE = '''
 using namespace spa;
 extern "C" void tiles_of(int lo, int hi, int sink, int window, int* out) { const KeyTiles t = key_tiles(lo, hi, sink, window); out[0] = t.sinks; out[1] = t.from; out[2] = t.n; }
 extern "C" int most(int q_len, int kv, int span, int sink, int window) { return most_key_tiles(q_len, kv, span, sink, window); }
-extern "C" int piece(long long work, int log_target, int min_tiles) { PagedPart p{}; p.log_target = log_target; p.min_tiles = min_tiles; return piece_of(work, p); }
+extern "C" int piece(long long work, int log_most, int min_tiles, int few) { PagedPart p{}; p.log_most = log_most; p.min_tiles = min_tiles; return few ? few_rows_piece(work, p) : shortest_piece(work, p); }
 extern "C" void share(int m, int log_m, int span, int G, int q_len, int kv, int sink, int window, int piece, int* out) {
     PagedPart p{}; p.m = m; p.log_m = log_m; p.span = span; p.row_lo = 0; p.row_hi = 0x7fffffff;
     const PagedShare s = paged_share(p, G, q_len, kv, sink, window, piece); out[0] = s.tiles; out[1] = s.keys; out[2] = s.splits; }
@@ -44,8 +44,8 @@ def test_every_seen_key_lies_in_a_tile_and_tiles_ascend(shim, sink, window, m, G
         assert longest <= keys <= max(longest + 3, (kv + 63) // 64 if not window else longest + 3)
 
 
-@pytest.mark.parametrize("log_target,min_tiles", [(9, 8), (11, 4)])
-def test_pieces_fill_the_target_and_stay_in_the_workspace(shim, log_target, min_tiles):
+@pytest.mark.parametrize("log_most,min_tiles,few", [(10, 2, 0), (11, 4, 1)])
+def test_pieces_stay_in_the_workspace(shim, log_most, min_tiles, few):
     out = (ctypes.c_int * 3)()
     for Hkv in (1, 8):
         for lens in ([131072], [131072, 90000, 1, 3], [100] * 60 + [50000], [8191] * 64, [10] * 4096, [2 ** 30]):
@@ -54,8 +54,9 @@ def test_pieces_fill_the_target_and_stay_in_the_workspace(shim, log_target, min_
                 shim.share(16, 4, 5, 4, 1, kv, 0, 0, 2 ** 24, out)
                 assert list(out) == [1, (kv + 63) // 64, 1]
                 work += out[0] * out[1] * Hkv
-            piece = shim.piece(ctypes.c_longlong(work), log_target, min_tiles)
+            piece = shim.piece(ctypes.c_longlong(work), log_most, min_tiles, few)
             assert piece >= min_tiles
+            assert not few or piece <= max(16, -(-work // 2 ** log_most))
             units = slots = 0
             for kv in lens:
                 shim.share(16, 4, 5, 4, 1, kv, 0, 0, piece, out)
@@ -64,4 +65,4 @@ def test_pieces_fill_the_target_and_stay_in_the_workspace(shim, log_target, min_
                 assert per * out[2] >= out[1] and per <= piece
                 units += out[0] * out[2] * Hkv
                 slots += out[0] * out[2] * Hkv if out[2] > 1 else 0
-            assert units <= 2 ** log_target + len(lens) * Hkv and slots <= 2 * 2 ** log_target
+            assert units <= 2 ** log_most + len(lens) * Hkv and slots <= 2 * 2 ** log_most
