@@ -206,19 +206,23 @@ __device__ __forceinline__ float sum_over_groups(float v) { v += __shfl_xor(v, 1
 // NV > 1: a workgroup makes the outputs of D / NV dims only, from all of K and its share of V.  A CU takes in about 12 bytes a
 // clock however many loads it has in flight (256 KB of a head: 22000 cycles of a call of 501 keys), so a call of few workgroups
 // is faster on NV times as many, although they read K NV times: 11.8 -> 9.2 us.
+// LDS of a workgroup: the wavefronts' outputs, references and denominators
+template <int D, int MF, int NW, int NV>
+constexpr int kFewLds = NW * 16 * (D / NV + 4) * 4 + 2 * NW * MF * 16 * 4;
 template <int D, int MF, bool MOD, bool SMALL, int NW, int NV>
-__global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, PagedPart part, unsigned units) {
+__device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& part, unsigned wg, unsigned units, char* lds) {
     constexpr int DS = D / 32;        // MFMAs of a logits tile
     constexpr int DV = D / NV;        // dims of the outputs
     constexpr int DT = DV / 16;       // 16-row tiles of O^T
     constexpr int PAD = DV + 4;
-    __shared__ __attribute__((aligned(16))) float s_o[NW][16][PAD];
-    __shared__ float s_m[NW][MF * 16], s_l[NW][MF * 16];
+    float (*const s_o)[16][PAD] = reinterpret_cast<float (*)[16][PAD]>(lds);
+    float (*const s_m)[MF * 16] = reinterpret_cast<float (*)[MF * 16]>(lds + NW * 16 * PAD * 4);
+    float (*const s_l)[MF * 16] = s_m + NW;
 
-    const int dv0 = NV > 1 ? (int)(blockIdx.x / units) * DV : 0;     // parts of a unit on one XCD where units are a multiple of 8
+    const int dv0 = NV > 1 ? (int)(wg / units) * DV : 0;     // parts of a unit on one XCD where units are a multiple of 8
     const Request first = request_at(a, threadIdx.x & 63);
     const int piece = part_piece<false>(a, part, first, threadIdx.x & 63);
-    const Share sh = share_of<false>(a, part, piece, first, NV > 1 ? blockIdx.x % units : blockIdx.x);
+    const Share sh = share_of<false>(a, part, piece, first, NV > 1 ? wg % units : wg);
     if (sh.b < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4;
@@ -436,6 +440,12 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, Page
     }
 }
 
+template <int D, int MF, bool MOD, bool SMALL, int NW, int NV>
+__global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, PagedPart part, unsigned units) {
+    __shared__ __attribute__((aligned(16))) char lds[kFewLds<D, MF, NW, NV>];
+    few_rows<D, MF, MOD, SMALL, NW, NV>(a, part, blockIdx.x, units, lds);
+}
+
 // ---------------------------------------------------------------------------------------------------------------
 // Many rows: 128 of them, 32 to a wavefront, S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_32x32x16_bf16 on key tiles that all
 // four share through LDS: the pipeline step of the sparse prefill's attention kernel (attn.hip: direct loads into a double
@@ -541,7 +551,7 @@ __device__ __forceinline__ void lds_dma16_from(uint32_t lds_addr, const void* la
 __device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 template <int D, int MODE, bool SMALL>
-__global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPart part) {
+__device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& part, unsigned wg, char* lds) {
     constexpr int NW = 4;
     constexpr int KT = kPagedTile;
     constexpr int DS = D / 16;          // MFMAs of one logits tile
@@ -555,13 +565,13 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
     constexpr int CHUNK_B = 32 * D * 2;
     constexpr int DTILE_B = 32 * KT * 2;
     static_assert(RPI * LPW == 16, "a wavefront loads 16 keys' rows, which lie in one page");
-    __shared__ __attribute__((aligned(1024))) uint16_t smemK[2][TILE];
-    __shared__ __attribute__((aligned(1024))) uint16_t smemV[2][TILE];
+    uint16_t (*const smemK)[TILE] = reinterpret_cast<uint16_t (*)[TILE]>(lds);      // K tile t in buffer t % 2
+    uint16_t (*const smemV)[TILE] = smemK + 2;                                      // V^T likewise
 
     const Request first = request_at(a, threadIdx.x & 63);
     const int piece = part_piece<true>(a, part, first, threadIdx.x & 63);
-    if (part.n_slots > 0 && blockIdx.x == 0 && threadIdx.x == 0) *part.piece = piece;
-    const Share sh = share_of<false>(a, part, piece, first, blockIdx.x);
+    if (part.n_slots > 0 && wg == 0 && threadIdx.x == 0) *part.piece = piece;
+    const Share sh = share_of<false>(a, part, piece, first, wg);
     if (sh.b < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, l32 = lane & 31;
@@ -883,6 +893,15 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, PagedPa
     }
 }
 
+// PAGES: 2, pages of 16 tokens; 1, of 32; 0, a key tile lies in one page
+template <int D, int MODE, int PAGES>
+__global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedArgs a, PagedPart many, unsigned many_grid, PagedPart few) {
+    __shared__ __attribute__((aligned(1024))) char lds[4 * kPagedTile * D * 2];
+    static_assert(kFewLds<D, 1, 4, 1> <= 4 * kPagedTile * D * 2, "few rows fit the tile buffers");
+    if (blockIdx.x < many_grid) many_rows<D, MODE, PAGES != 0>(a, many, blockIdx.x, lds);
+    else few_rows<D, 1, MODE != kPlain, PAGES == 2, 4, 1>(a, few, blockIdx.x - many_grid, 0, lds);
+}
+
 // ---------------------------------------------------------------------------------------------------------------
 // Merge of the pieces' results: out = sum_s w_s out_s / sum_s w_s, w_s = 2^(lse_s - max).  A wavefront makes D / NV dims of a row, 64 pieces
 // at a time: a lane has the weight of one, then DV / 4 lanes read a piece's values, 64 / (DV / 4) pieces side by side.  NV = 4 for few
@@ -989,23 +1008,27 @@ void launch_few(const PagedArgs& a, const PagedPart& part, unsigned units, hipSt
 
 template <int D>
 hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts& parts, hipStream_t st) {
-    if (parts.few.m) {
-        const int64_t grid = most_units(d, parts.few);
-        if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-        if (parts.few.m == 32) launch_few<D, 2, 4, 1>(a, parts.few, (unsigned)grid, st);
-        else if (grid <= 64) launch_few<D, 1, 8, 4>(a, parts.few, (unsigned)grid, st);
-        else launch_few<D, 1, 4, 1>(a, parts.few, (unsigned)grid, st);
+    // A call with requests of both kinds runs them side by side, the many-row workgroups first: the ones wait for the matrix cores, the
+    // others for the memory (mixed step 431 -> 399 us, 10 short prompts and single tokens 24.8 -> 19.3).  With 17 to 32 query heads of a KV head, one after the other.
+    const bool both = parts.many.m && parts.few.m == 16;
+    const int64_t few_grid = parts.few.m ? most_units(d, parts.few) : 0, many_grid = parts.many.m ? most_units(d, parts.many) : 0;
+    if (few_grid + many_grid > 0x7fffffffll) return hipErrorInvalidValue;
+    if (parts.few.m && !both) {
+        if (parts.few.m == 32) launch_few<D, 2, 4, 1>(a, parts.few, (unsigned)few_grid, st);
+        else if (few_grid <= 64) launch_few<D, 1, 8, 4>(a, parts.few, (unsigned)few_grid, st);
+        else launch_few<D, 1, 4, 1>(a, parts.few, (unsigned)few_grid, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (parts.many.m) {
-        const int64_t grid = most_units(d, parts.many);
-        if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, st, a, parts.many); };
+        const auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(many_grid + (both ? few_grid : 0))), dim3(256), 0, st, a, parts.many, (unsigned)many_grid, parts.few);
+        };
         const auto with_pages = [&](auto mode) {
             constexpr int MODE = decltype(mode)::value;
-            if (a.log_p < 6) go(paged_many_kernel<D, MODE, true>);
-            else go(paged_many_kernel<D, MODE, false>);
+            if (a.log_p == 4) go(paged_attn_kernel<D, MODE, 2>);
+            else if (a.log_p == 5) go(paged_attn_kernel<D, MODE, 1>);
+            else go(paged_attn_kernel<D, MODE, 0>);
         };
         if (a.cap > 0.f && a.slopes != nullptr) with_pages(IC<kCappedSlopes>{});
         else if (a.cap > 0.f) with_pages(IC<kCapped>{});
