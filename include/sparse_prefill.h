@@ -452,9 +452,10 @@ int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const 
  *   out = sum_j softmax(x)_j v_j
  * in fp32 with bf16 matrix products; out [n_tokens, n_q_heads, head_dim] bf16.  slopes_or_null: n_q_heads fp32
  * on the device (bias by distance).  lse_or_null: [n_tokens, n_q_heads] fp32, ln sum_j e^x_j.  A query that
- * sees no key (kv_lens[b] = 0, or a position below 0) gets zeros and -inf.  Values behind the last key that a
- * query sees never reach it, whatever they are, when it is its request's only one; among the queries of one
- * request an infinite or NaN value may also reach queries up to 127 tokens away from those that see it.
+ * sees no key (kv_lens[b] = 0, or a position below 0) gets zeros and -inf.  What lies behind a request's last key, and
+ * what no query of the call sees, may be anything, NaN too.  Masked keys have no influence otherwise either, with one
+ * exception: where a request has several new tokens, an infinite or NaN VALUE that one of them sees may also reach
+ * those up to 127 tokens before or behind it that do not (their weight for it is 0, and 0 * inf is NaN).
  * ws: spa_paged_workspace_bytes() bytes, 256-byte aligned; its contents need not survive between calls, calls
  * that overlap in time need one each. */
 int sparse_prefill_paged_attn(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,
