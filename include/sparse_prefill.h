@@ -453,9 +453,8 @@ int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const 
  * in fp32 with bf16 matrix products; out [n_tokens, n_q_heads, head_dim] bf16.  slopes_or_null: n_q_heads fp32
  * on the device (bias by distance).  lse_or_null: [n_tokens, n_q_heads] fp32, ln sum_j e^x_j.  A query that
  * sees no key (kv_lens[b] = 0, or a position below 0) gets zeros and -inf.  What lies behind a request's last key, and
- * what no query of the call sees, may be anything, NaN too.  Masked keys have no influence otherwise either, with one
- * exception: where a request has several new tokens, an infinite or NaN VALUE that one of them sees may also reach
- * those up to 127 tokens before or behind it that do not (their weight for it is 0, and 0 * inf is NaN).
+ * what no query of the call sees, may be anything, NaN too; a key that a query does not see has no influence on it,
+ * whatever its key and value are.  Infinite and NaN values that it sees reach it as arithmetic has it.
  * ws: spa_paged_workspace_bytes() bytes, 256-byte aligned; its contents need not survive between calls, calls
  * that overlap in time need one each. */
 int sparse_prefill_paged_attn(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,

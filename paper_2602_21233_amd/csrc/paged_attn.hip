@@ -168,6 +168,18 @@ __device__ __forceinline__ int tiles_of_piece(const PagedShare& s) { return (int
 // K rows are assigned to the first product's rows such that the weights are the second one's operand as they are.  Bound
 // by HBM: nothing is shared between the wavefronts, so there is no LDS in the loop and no barrier.
 
+// A pair of bf16 values: whether either is infinite or NaN (its exponent is all ones); the pair with such a one as 0.
+__device__ __forceinline__ bool not_finite(uint32_t pair) { return (((pair & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0; }
+__device__ __forceinline__ uint32_t finite_part(uint32_t pair) {
+    return pair & (((pair & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((pair & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u));
+}
+// Which keys the query at position pos sees, and whether one of 32 or 64 keys from key0 on is hidden from one of the positions
+// lo .. hi
+__device__ __forceinline__ bool sees(const PagedArgs& a, int pos, int key) { return key <= pos && (a.window == 0 || pos - key < a.window || key < a.sink); }
+__device__ __forceinline__ bool hides(const PagedArgs& a, int lo, int hi, int key0, int n) {
+    return key0 + n - 1 > lo || (a.window > 0 && key0 + n - 1 >= a.sink && key0 <= hi - a.window);
+}
+
 // base-2 logits of a lane: what the options make of scaled products
 struct Logits {
     float c;                          // scale * log2 e
@@ -298,9 +310,11 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
 #pragma unroll
         for (int t = 0; t < DT; ++t) ch.v[t] = *reinterpret_cast<const u32x4*>(vp + 16 * t * page);
     };
+    bool put_back = false;                                      // of this wavefront
     auto attend = [&](int c, Chunk& ch) __attribute__((always_inline)) {
         const int key0 = key_of(c);
-        // keys that no row of the tile sees: behind its last position, or between the sinks and its first window
+        // Values of keys that no row of the tile sees (behind its last position, or between the sinks and its first window) may be
+        // anything, NaN too, and a weight of 0 would not hide them: they become 0.
         const int gone_lo = a.sink, gone_hi = a.window > 0 ? pos_lo - a.window + 1 : 0;       // [gone_lo, gone_hi)
         if (key0 + 31 > pos_hi || (key0 + 31 >= gone_lo && key0 < gone_hi)) {
             const int key = key0 + 8 * g;
@@ -314,7 +328,22 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
 #pragma unroll
             for (int t = 0; t < DT; ++t) ch.v[t] &= keep;
         }
-        const bool masked = key0 + 31 > pos_lo || (a.window > 0 && key0 + 31 >= a.sink && key0 <= pos_hi - a.window);
+        const bool masked = hides(a, pos_lo, pos_hi, key0, 32);
+        // Where some rows see a key and others do not, its infinite and NaN values are taken out and come back at the end.
+        if (masked && pos_lo != pos_hi) {
+            bool odd = false;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) odd |= not_finite(ch.v[t][x]);
+            if (__any(odd)) {
+                put_back = true;
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) ch.v[t][x] = finite_part(ch.v[t][x]);
+            }
+        }
 #pragma unroll
         for (int f = 0; f < MF; ++f) {
             f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
@@ -333,8 +362,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
             if (masked) {
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
-                    const int b = back - r;
-                    if (b < 0 || (a.window > 0 && b >= a.window && pos[f] - b >= a.sink)) x[r] = -INFINITY;
+                    if (!sees(a, pos[f], pos[f] - back + r)) x[r] = -INFINITY;
                 }
             }
             const float mr = m[f] == -INFINITY ? 0.f : m[f];
@@ -352,7 +380,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
                 mx = max_over_groups(mx);
                 const float lq = sum_over_groups(l[f]);
                 const float m_new = fmaxf(m[f] == -INFINITY ? m[f] : m[f] + (lq > 1.f ? __log2f(lq) : 0.f), mx);
-                const float alpha = m[f] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[f] - m_new);
+                const float alpha = m[f] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[f] - m_new);
                 m[f] = m_new;
                 l[f] *= alpha;
 #pragma unroll
@@ -382,6 +410,31 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
             load(c, pg, one);
             pg = pages_of(c + NW);                              // one chunk ahead
             attend(c, one);
+        }
+    }
+
+    if (put_back) {                                             // rare: infinite and NaN values, for the rows that see them
+        for (int cc = 2 * cut * per + wave; cc < c_end; cc += NW) {
+            const int key0 = key_of(cc);
+            if (!hides(a, pos_lo, pos_hi, key0, 32)) continue;
+            for (int key = key0; key < key0 + 32 && key <= pos_hi; ++key) {
+                const uint16_t* const src = a.vt + page_of(key) * a.vp_p + kvh * a.vp_h + (int64_t)dv0 * page + (key & (page - 1));
+                int step = page;                                // unknown to the compiler, which would keep all the offsets in registers
+                asm volatile("" : "+s"(step));
+#pragma unroll
+                for (int f = 0; f < MF; ++f) {
+                    if (!sees(a, pos[f], key)) continue;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const uint32_t u = src[(16 * t + 4 * g + r) * step];
+                            if (not_finite(u)) o[f][t][r] += __uint_as_float(u << 16);
+                        }
+                        asm volatile("" ::: "memory");           // four loads at a time: the registers are for the usual case
+                    }
+                }
+            }
         }
     }
 
@@ -441,7 +494,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
 }
 
 template <int D, int MF, bool MOD, bool SMALL, int NW, int NV>
-__global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedArgs a, PagedPart part, unsigned units) {
+__global__ __launch_bounds__(64 * NW, MF > 1 ? 2 : D == 64 ? 5 : 3) void paged_few_kernel(PagedArgs a, PagedPart part, unsigned units) {
     __shared__ __attribute__((aligned(16))) char lds[kFewLds<D, MF, NW, NV>];
     few_rows<D, MF, MOD, SMALL, NW, NV>(a, part, blockIdx.x, units, lds);
 }
@@ -591,17 +644,25 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     const int row = min(row0 + 32 * wave + l32, last_row);                    // rows past the last repeat it; they are not stored
     const bool valid = row0 + 32 * wave + l32 <= last_row;
     const int token = row / a.G, head = kvh * a.G + row % a.G, pos = pos0 + token;
-    uint16_t* const orow = a.out + (int64_t)(sh.r.first + token) * a.o_t + head * a.o_h;
-    float* const po = part.o + ((int64_t)slot * kManyRows + 32 * wave + l32) * D;
-    float* const plse = part.lse + (int64_t)slot * kManyRows + 32 * wave + l32;
+    auto store_lse = [&](int at, float lse2) {                                // at: the row, counted from the workgroup's first
+        if (partial) {
+            part.lse[(int64_t)slot * kManyRows + at] = lse2;
+        } else if (a.lse != nullptr) {
+            const int r = row0 + at;
+            a.lse[(int64_t)(sh.r.first + r / a.G) * a.Hq + kvh * a.G + r % a.G] = lse2 * kLn2;
+        }
+    };
+    auto out_row = [&](int at) {
+        const int r = row0 + at;
+        return a.out + (int64_t)(sh.r.first + r / a.G) * a.o_t + (kvh * a.G + r % a.G) * a.o_h;
+    };
     if (n_st <= 0) {                                                          // no key in sight (of this piece)
         if (valid && half == 0) {
-            if (partial) {
-                *plse = -INFINITY;
-            } else {
+            store_lse(32 * wave + l32, -INFINITY);
+            if (!partial) {
+                uint16_t* const orow = out_row(32 * wave + l32);
 #pragma unroll
                 for (int x = 0; x < D / 8; ++x) *reinterpret_cast<u32x4*>(orow + 8 * x) = u32x4{0u, 0u, 0u, 0u};
-                if (a.lse != nullptr) a.lse[(int64_t)(sh.r.first + token) * a.Hq + head] = -INFINITY;
             }
         }
         return;
@@ -638,6 +699,18 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     }
     const uint32_t k_dst = lds_address(&smemK[0][0]) + wave * LPW * 1024;
     const uint32_t v_dst = lds_address(&smemV[0][0]) + wave * LPW * 1024;
+    // With head_dim 64 (two loads of a wavefront) the second offset follows from the first, 8 rows on with bit 2 of the chunk turned:
+    // one register less for each operand
+    auto second = [&](const uint32_t (&off)[LPW], auto x_tag, int rows_b) {
+        constexpr int X = decltype(x_tag)::value;
+        if constexpr (D == 64 && X == 1) {
+            uint32_t first = off[0];
+            asm volatile("" : "+v"(first));
+            return (first ^ 64u) + (uint32_t)rows_b;
+        } else {
+            return off[X];
+        }
+    };
     auto issue_k = [&](auto buf_tag, int t, const Pages& pg) {
         constexpr int BUF = decltype(buf_tag)::value;
         const int key = key_of(t) + 16 * wave;                                // this wavefront's 16 keys
@@ -646,7 +719,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         const char* const src = kbase + 2 * ((int64_t)id * a.kp_p + (key & (page - 1)) * D);
         static_for<LPW>([&](auto x_tag) {
             constexpr int X = decltype(x_tag)::value;
-            lds_dma16<BUF * TILE_B + X * 1024>(k_dst, k_offb[X], src);
+            lds_dma16<BUF * TILE_B + X * 1024>(k_dst, second(k_offb, x_tag, RPI * D * 2), src);
         });
     };
     auto issue_v = [&](auto buf_tag, int t, const Pages& pg) {
@@ -656,7 +729,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
             const char* const src = vbase0 + 2 * ((int64_t)pg.id[0] * a.vp_p + (key0 & (page - 1)));
             static_for<LPW>([&](auto x_tag) {
                 constexpr int X = decltype(x_tag)::value;
-                lds_dma16<BUF * TILE_B + X * 1024>(v_dst, v_offb[X], src);
+                lds_dma16<BUF * TILE_B + X * 1024>(v_dst, second(v_offb, x_tag, 16 * page), src);
             });
         } else {
             const char* src[2];
@@ -673,23 +746,37 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         }
     };
     // Values of keys that no row of the workgroup sees may be anything, NaN too, and a weight of 0 would not hide them: they
-    // become 0 in LDS.  A wavefront does so for what it has loaded itself, before the barrier that publishes the tile.
+    // become 0 in LDS.  Where some rows see a key and others do not, its infinite and NaN values are taken out and come back at the
+    // end.  A wavefront does so for what it has loaded itself, before the barrier that publishes the tile.
     const int gone_hi = a.window > 0 ? pos_lo - a.window + 1 : 0;             // keys sink .. gone_hi - 1 are out of sight
+    uint32_t put_back = 0;
     auto clear_unseen = [&](auto buf_tag, int t) {
         constexpr int BUF = decltype(buf_tag)::value;
         const int key0 = key_of(t);
-        if (key0 + KT - 1 <= pos_hi && !(key0 + KT - 1 >= a.sink && key0 < gone_hi)) return;
+        if (!hides(a, pos_lo, pos_hi, key0, KT)) return;
+        const bool unseen = key0 + KT - 1 > pos_hi || (key0 + KT - 1 >= a.sink && key0 < gone_hi);
+        u32x4* const at = reinterpret_cast<u32x4*>(reinterpret_cast<char*>(&smemV[BUF][0]) + wave * LPW * 1024 + lane * 16);
+        int of = lane;                                      // the chunks found anew, not kept in registers
+        asm volatile("" : "+v"(of));
 #pragma unroll
         for (int x = 0; x < LPW; ++x) {
-            u32x4* const at = reinterpret_cast<u32x4*>(reinterpret_cast<char*>(&smemV[BUF][0]) + (wave * LPW + x) * 1024 + lane * 16);
-            u32x4 v = *at;
+            const int chunk = (of & 7) ^ swz_v(8 * (wave * LPW + x) + (of >> 3));
+            u32x4 v = at[64 * x];
+            bool odd = false;
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-                const int ka = key0 + 8 * v_chunk[x % 2] + 2 * y, kb = ka + 1;
+                const int ka = key0 + 8 * chunk + 2 * y, kb = ka + 1;
                 v[y] &= (ka <= pos_hi && !(ka >= a.sink && ka < gone_hi) ? 0xffffu : 0u) |
                         (kb <= pos_hi && !(kb >= a.sink && kb < gone_hi) ? 0xffff0000u : 0u);
+                odd |= not_finite(v[y]);
             }
-            *at = v;
+            const bool some = __any(odd);
+            if (some) {
+                put_back = 1;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) v[y] = finite_part(v[y]);
+            }
+            if (unseen || some) at[64 * x] = v;
         }
     };
 
@@ -719,7 +806,8 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     const char* const ldsV = reinterpret_cast<const char*>(&smemV[0][0]);
     auto lds16 = [](const char* p) { return *reinterpret_cast<const bf16x8*>(p); };
 
-    // Running softmax, in base 2.  m: the reference; -inf until the row has seen a key, and then limit = -1 sends it to the slow path.
+    // Running softmax, in base 2.  m: the reference; l: the lane's share of the denominator, infinite (which sends the row to the slow path)
+    // until the row has seen a key.
     f32x16 oacc[DT];
 #pragma unroll
     for (int dc = 0; dc < DT; ++dc)
@@ -730,12 +818,10 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     cw.cap2 = a.cap * kLog2e;
     cw.k = ChunkWeights<MODE>::kCap ? 2.f * cw.c / a.cap : 0.f;
     cw.slope2 = ChunkWeights<MODE>::kBias ? a.slopes[head] * kLog2e : 0.f;
-    float m = -INFINITY, m0 = 0.f, l = 0.f, limit = -1.f;                     // m0: m, or 0 where that is -inf
+    float m = 0.f, l = INFINITY;
     const int wave_row = row0 + 32 * wave;                                    // wave-uniform bounds of this wavefront's rows
     const int wave_lo = pos0 + min(wave_row, last_row) / a.G, wave_hi = pos0 + min(wave_row + 31, last_row) / a.G;
-    auto needs_mask = [&](int key0) {
-        return key0 + 31 > wave_lo || (a.window > 0 && key0 + 31 >= a.sink && key0 <= wave_hi - a.window);
-    };
+    auto needs_mask = [&](int key0) { return hides(a, wave_lo, wave_hi, key0, 32); };
     // Slow path of a chunk: masks, and a reference that makes its weights at most 1 and the denominator so far about 1 or less.
     // For the first chunk, masked ones, and where the denominator passed the limit.
     auto slow_weights = [&](const f32x16& s, int key0, bf16x8& p0, bf16x8& p1) __attribute__((always_inline)) {
@@ -747,8 +833,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         if (needs_mask(key0)) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int b = back - 16 * (r >> 3) - (r & 7);
-                if (b < 0 || (a.window > 0 && b >= a.window && pos - b >= a.sink)) {
+                if (!sees(a, pos, pos - back + ChunkWeights<MODE>::key_of(r))) {
                     hidden |= 1u << r;
                     x[r] = -INFINITY;
                 }
@@ -759,13 +844,11 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
         mx = fmaxf(mx, other_half(mx));
         const float lq = l + other_half(l);
-        const bool first = m == -INFINITY;
-        const float m_new = fmaxf(first ? m : m + (lq > 1.f ? __log2f(lq) : 0.f), mx);
-        const float alpha = first ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
-        m = m_new;
-        m0 = m == -INFINITY ? 0.f : m;
-        limit = m == -INFINITY ? -1.f : kRescaleAt;
-        l *= alpha;
+        const bool first = l == INFINITY;
+        const float m_new = fmaxf(first ? -INFINITY : m + (lq > 1.f ? __log2f(lq) : 0.f), mx);
+        const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new == -INFINITY ? 0.f : m_new;
+        l = m_new == -INFINITY ? INFINITY : first ? 0.f : l * alpha;
 #pragma unroll
         for (int dc = 0; dc < DT; ++dc)
 #pragma unroll
@@ -773,8 +856,8 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         f32x8 w0, w1;
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-            w0[r] = (hidden >> r) & 1 ? 0.f : __builtin_amdgcn_exp2f(cw.exponent(s[r], r, m0, -back));
-            w1[r] = (hidden >> (8 + r)) & 1 ? 0.f : __builtin_amdgcn_exp2f(cw.exponent(s[8 + r], 8 + r, m0, -back));
+            w0[r] = (hidden >> r) & 1 ? 0.f : __builtin_amdgcn_exp2f(cw.exponent(s[r], r, m, -back));
+            w1[r] = (hidden >> (8 + r)) & 1 ? 0.f : __builtin_amdgcn_exp2f(cw.exponent(s[8 + r], 8 + r, m, -back));
         }
 #pragma unroll
         for (int r = 0; r < 8; ++r) l += w0[r] + w1[r];
@@ -792,15 +875,23 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     auto step = [&](auto kb_tag, auto vb_tag, auto kc_tag, int key0, const f32x16& s_cur, f32x16& s_nxt, const bf16x8& pc0, const bf16x8& pc1,
                     bf16x8& pn0, bf16x8& pn1, bf16x8 (&f)[4]) __attribute__((always_inline)) {
         constexpr int KB = decltype(kb_tag)::value, VB = decltype(vb_tag)::value, KC = decltype(kc_tag)::value;
-        cw.at(m0, key0 + 8 * half - pos);
+        cw.at(m, key0 + 8 * half - pos);
         const char* const vbase = ldsV + VB * TILE_B;
+        int vslice[2] = {vofs[2 * KC], vofs[2 * KC + 1]};      // the second chunk's 8-key slices have bit 2 turned: found from the first's
+        if constexpr (D == 64 && KC == 1) {
+            vslice[0] = vofs[0];
+            vslice[1] = vofs[1];
+            asm volatile("" : "+v"(vslice[0]), "+v"(vslice[1]));
+            vslice[0] ^= 64;
+            vslice[1] ^= 64;
+        }
         auto operand = [&](auto j_tag) {            // operand j of this step (j < NG) or of the next one
             constexpr int J = decltype(j_tag)::value;
             constexpr int j = J % NG;
             constexpr int kc = KC + J / NG;
             const char* const kb2 = ldsK + KB * TILE_B + kc * CHUNK_B;
             if constexpr (j % 2 == 0) return lds16(kb2 + kofs[j / 2]);
-            else return lds16(vbase + vofs[2 * kc + (j / 2) / DT] + ((j / 2) % DT) * DTILE_B);
+            else return lds16(vbase + (kc == KC ? vslice[(j / 2) / DT] : vofs[2 * kc + (j / 2) / DT]) + ((j / 2) % DT) * DTILE_B);
         };
         f32x8 e;
         float l_new = l;
@@ -813,7 +904,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         };
         SPA_FENCE();
         static_for<NG>([&](auto g_tag) { group(g_tag); });
-        if (needs_mask(key0) || __any(!(l_new < limit))) slow_weights(s_cur, key0, pn0, pn1);
+        if (needs_mask(key0) || __any(!(l_new < kRescaleAt))) slow_weights(s_cur, key0, pn0, pn1);
         else l = l_new;
     };
 
@@ -863,39 +954,59 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         if (++t == n_st) break;
     }
 
+    // Infinite and NaN values that were taken out, for the rows that see them: rare, so it looks through all the tiles again
+    __syncthreads();
+    uint32_t* const flags = reinterpret_cast<uint32_t*>(lds);
+    if (lane == 0) flags[wave] = put_back;
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3])) {
+        for (int t = 0; t < n_st; ++t) {
+            const int key0 = key_of(t);
+            if (!hides(a, pos_lo, pos_hi, key0, KT)) continue;
+            for (int key = key0; key < key0 + KT && key <= pos_hi; ++key) {
+                const uint16_t* const src = a.vt + page_of(key) * a.vp_p + kvh * a.vp_h + (key & (page - 1));
+                int step = page;                                // unknown to the compiler, which would keep all the offsets in registers
+                asm volatile("" : "+s"(step));
+                if (!sees(a, pos, key)) continue;
+#pragma unroll
+                for (int dc = 0; dc < DT; ++dc)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t u = src[(32 * dc + 8 * (r >> 2) + 4 * half + (r & 3)) * step];
+                        if (not_finite(u)) oacc[dc][r] += __uint_as_float(u << 16);
+                        if (r % 4 == 3) asm volatile("" ::: "memory");   // four loads at a time: the registers are for the usual case
+                    }
+            }
+        }
+    }
+
     const float lt = l + other_half(l);
-    const bool none = m == -INFINITY && lt == 0.f;         // a row that sees no key; NaN is not none
+    const bool none = l == INFINITY;         // a row that sees no key; NaN is not none
     const float inv = none ? 0.f : 1.f / lt;
     const float lse2 = none ? -INFINITY : m + __log2f(lt);
-    if (!valid) return;
-    if (partial) {
+    int at = 32 * wave + l32;
+    asm volatile("" : "+v"(at));                           // found anew, not kept in registers all the way
+    if (row0 + at > last_row) return;
+    if (half == 0) store_lse(at, lse2);
+    uint16_t* const orow = out_row(at);
+    float* const po = part.o + ((int64_t)slot * kManyRows + at) * D;
 #pragma unroll
-        for (int dc = 0; dc < DT; ++dc)
+    for (int dc = 0; dc < DT; ++dc)
 #pragma unroll
-            for (int rq = 0; rq < 4; ++rq) {
-                f32x4 o4;
+        for (int rq = 0; rq < 4; ++rq) {
+            f32x4 o4;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) o4[x] = oacc[dc][4 * rq + x] * inv;
-                *reinterpret_cast<f32x4*>(po + 32 * dc + 8 * rq + 4 * half) = o4;
-            }
-        if (half == 0) *plse = lse2;
-    } else {
-#pragma unroll
-        for (int dc = 0; dc < DT; ++dc)
-#pragma unroll
-            for (int rq = 0; rq < 4; ++rq) {
-                f32x4 o4;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) o4[x] = oacc[dc][4 * rq + x] * inv;
-                *reinterpret_cast<bf16x4*>(orow + 32 * dc + 8 * rq + 4 * half) = __builtin_convertvector(o4, bf16x4);
-            }
-        if (a.lse != nullptr && half == 0) a.lse[(int64_t)(sh.r.first + token) * a.Hq + head] = lse2 * kLn2;
-    }
+            for (int x = 0; x < 4; ++x) o4[x] = oacc[dc][4 * rq + x] * inv;
+            const int d = 32 * dc + 8 * rq + 4 * half;
+            if (partial) *reinterpret_cast<f32x4*>(po + d) = o4;
+            else *reinterpret_cast<bf16x4*>(orow + d) = __builtin_convertvector(o4, bf16x4);
+        }
 }
 
-// PAGES: 2, pages of 16 tokens; 1, of 32; 0, a key tile lies in one page
+// PAGES: 2, pages of 16 tokens; 1, of 32; 0, a key tile lies in one page.  With head_dim 64 and a key tile in one page three wavefronts share
+// a SIMD (prompts of 4000 tokens with slopes 228 -> 197 us); cap and slopes together do not leave the registers for it.
 template <int D, int MODE, int PAGES>
-__global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedArgs a, PagedPart many, unsigned many_grid, PagedPart few) {
+__global__ __launch_bounds__(256, D == 64 && PAGES == 0 && MODE != kCappedSlopes ? 3 : 2) void paged_attn_kernel(PagedArgs a, PagedPart many, unsigned many_grid, PagedPart few) {
     __shared__ __attribute__((aligned(1024))) char lds[4 * kPagedTile * D * 2];
     static_assert(kFewLds<D, 1, 4, 1> <= 4 * kPagedTile * D * 2, "few rows fit the tile buffers");
     if (blockIdx.x < many_grid) many_rows<D, MODE, PAGES != 0>(a, many, blockIdx.x, lds);

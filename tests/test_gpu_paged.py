@@ -284,6 +284,31 @@ def test_attn_of_infinite_and_nan_values(spa):
     assert torch.isinf(got[0, :, 5]).all() and torch.equal(got[0, :, :5], clean[0, :, :5]) and torch.equal(got[0, :, 6:], clean[0, :, 6:])
 
 
+@pytest.mark.parametrize("head_dim,page,q_heads", [(64, 16, 4), (128, 64, 4), (128, 32, 2), (64, 128, 24)])
+@pytest.mark.parametrize("ctx,new,window,sink", [(100, 4, 0, 0), (300, 7, 40, 3), (5, 150, 0, 0), (70, 150, 33, 70), (700, 130, 300, 10), (2000, 40, 0, 0)])
+def test_values_that_are_not_finite_reach_those_who_see_them_and_no_others(spa, ctx, new, window, sink, head_dim, page, q_heads):
+    step = oracle.Step(new, [ctx], [new], page=page, q_heads=q_heads, kv_heads=1, head_dim=head_dim)
+    call = lambda: spa.paged_attn(step.q.cuda(), step.k_pages.cuda(), step.vt_pages.cuda(), step.table.cuda(), _i32(step.starts), _i32(step.kv_lens),  # noqa: E731
+                                  max_new_tokens=new, window_tokens=window, n_sink_tokens=sink).float().cpu()
+    clean, n = call(), ctx + new
+    odd = {n - 1: (3, math.inf), n - new // 2: (9, math.nan), n - new + 1: (60, -math.inf), max(0, n - new - window - 1): (17, math.inf), 1: (33, -math.inf),
+           n - 3: (3, -math.inf)}
+    for key, (d, value) in odd.items():
+        step.vt_pages[step.table[0, key // page], 0, d, key % page] = value
+    got = call()
+    for i in range(new):
+        pos, want = ctx + i, clean[i].clone()
+        seen = {key for key in odd if key <= pos and (window == 0 or pos - key < window or key < sink)}
+        for d in {odd[key][0] for key in seen}:
+            mixed = sum(odd[key][1] for key in seen if odd[key][0] == d)
+            if math.isnan(mixed):
+                assert torch.isnan(got[i, :, d]).all()
+            else:                                                  # a weight of 0 makes NaN of an infinite value
+                assert (torch.isnan(got[i, :, d]) | (got[i, :, d] == mixed)).all(), (i, d)
+            want[:, d] = got[i, :, d]
+        assert torch.equal(want.nan_to_num(7.0), got[i].nan_to_num(7.0)), i
+
+
 def test_attn_of_malformed_lengths_stays_inside(spa):
     """Unspecified rows, but every other request keeps its bits."""
     step = oracle.Step(6, [100, 50, 80], [1, 1, 1], q_heads=4, kv_heads=1, head_dim=64)
