@@ -405,7 +405,8 @@ typedef struct spa_paged_params {
     int32_t n_sink_tokens;  /* >= 0 } with window_tokens = w > 0 the query at position i sees the keys */
     int32_t window_tokens;  /* >= 0 } j <= i with i - j < w or j < n_sink_tokens (the A-shape of
                                Sec. 4.1.1, by tokens); with w = 0 every key j <= i              */
-    float softcap;          /* 0: none.  c > 0: a scaled logit s becomes c * tanh(s / c)        */
+    float softcap;          /* 0: none.  c in (0, 65536]: a scaled logit s becomes c * tanh(s / c), to
+                               about c * 2^-22                                                  */
     int64_t table_stride;   /* >= max_pages elements                                            */
     int64_t q_stride[2];    /* elements: token, head; the head_dim axis is contiguous           */
     int64_t k_stride[2];

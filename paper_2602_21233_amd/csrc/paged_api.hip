@@ -20,7 +20,7 @@ int check_paged(const spa_paged_params* p) {
     if (p->max_pages < 1 || (int64_t)p->max_pages * p->page_size > kMostTokens) return SPA_ERR_BAD_SHAPE;
     if (p->n_tokens > (1 << 24) || (int64_t)p->n_tokens * p->n_q_heads > 0x7fffffffll || p->max_new_tokens < 0) return SPA_ERR_BAD_SHAPE;
     if (!(p->softmax_scale >= 0.0f) || isinf(p->softmax_scale)) return SPA_ERR_BAD_SHAPE;
-    if (p->n_sink_tokens < 0 || p->window_tokens < 0 || !(p->softcap >= 0.0f) || isinf(p->softcap)) return SPA_ERR_BAD_PATTERN;
+    if (p->n_sink_tokens < 0 || p->window_tokens < 0 || !(p->softcap >= 0.0f) || p->softcap > 65536.0f) return SPA_ERR_BAD_PATTERN;
     return SPA_OK;
 }
 

@@ -77,6 +77,8 @@ def _rows(name, t, device, n, heads, dim):
 
 def _cache(k_pages, vt_pages):
     """(n_pages, n_kv_heads, page_size, head_dim, K's page and head strides, V's, device)"""
+    if k_pages.dim() != 4:
+        raise TypeError("k_pages must be [n_pages, n_kv_heads, page_size, head_dim]")
     n, h, p, d = k_pages.shape
     device = k_pages.device
     if k_pages.dtype is not _BF16 or vt_pages.dtype is not _BF16 or not k_pages.is_cuda or vt_pages.device != device:
@@ -146,6 +148,8 @@ def paged_attn(q, k_pages, vt_pages, block_table, q_starts, kv_lens, max_new_tok
     max_new_tokens: the most new tokens of a request, where the host knows it; slopes: fp32 [n_q_heads], bias by distance.
     Rows of padding are left as they are in `out` (as allocated where none is given)."""
     n, h, page, d, k0, k1, v0, v1, dev = _cache(k_pages, vt_pages)
+    if q.dim() != 3 or kv_lens.dim() != 1:
+        raise TypeError("q must be [n_tokens, n_q_heads, head_dim] and kv_lens [batch]")
     B = kv_lens.shape[0]
     T, Hq, _ = q.shape
     for name, t, many in (("q_starts", q_starts, B + 1), ("kv_lens", kv_lens, B)):

@@ -203,6 +203,24 @@ def test_attn_with_capped_logits_and_bias_by_distance(spa, ctx, new, softcap, sl
     _attn_close(spa, step, new=max(new), softcap=softcap, slopes=s, window=window, sink=3)
 
 
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("softcap,slopes", [(0.0, False), (0.0, True), (25.0, False), (25.0, True)])
+def test_attn_of_every_kernel(spa, softcap, slopes, page, head_dim):
+    """Requests of few and of many rows in one call, only few, only many; with and without cuts."""
+    s = torch.exp2(-torch.arange(1.0, 5.0)) if slopes else None
+    for ctx, new in (([130, 0, 700], [140, 33, 1]), ([200, 33, 900], [1, 1, 2]), ([650], [90])):
+        step = oracle.Step(page + len(ctx), ctx, new, q_heads=4, kv_heads=1, page=page, head_dim=head_dim, peak=2.0)
+        _attn_close(spa, step, new=max(new), softcap=softcap, slopes=s)
+
+
+@pytest.mark.parametrize("softcap", [1e-38, 1e-44, 65536.0])
+def test_attn_of_the_smallest_and_largest_cap(spa, softcap):
+    step = oracle.Step(1, [100, 0], [1, 40], q_heads=4, kv_heads=1, head_dim=64)
+    step.q[0] = 0.0
+    _attn_close(spa, step, new=40, softcap=softcap)
+
+
 def test_attn_with_wild_slopes(spa):
     """Slopes that favour far keys, none, large ones."""
     step = oracle.Step(5, [400, 90], [1, 70], q_heads=4, kv_heads=1, head_dim=64)
@@ -244,6 +262,24 @@ def test_attn_over_a_long_cache_is_cut_and_merged(spa, long):
     step = oracle.Step(long, [20000, 30, 5000, 0], [long, 1, 1, 2], q_heads=4, kv_heads=1, head_dim=64, page=128)
     _attn_close(spa, step, new=long)
     _attn_close(spa, step, new=long, window=9000, sink=300)
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("q_heads", [4, 16, 20, 32, 40])
+def test_attn_of_one_long_request_is_cut_and_merged(spa, q_heads, head_dim):
+    """One KV head: few workgroups, that make a part of the dims each, of 16, 32 or more rows."""
+    for ctx in (3000, 600, 511):
+        step = oracle.Step(q_heads, [ctx], [1], q_heads=q_heads, kv_heads=1, head_dim=head_dim, page=32)
+        _attn_close(spa, step, new=1)
+        _attn_close(spa, step, new=1, softcap=20.0, window=700, sink=70)
+
+
+def test_attn_of_two_thousand_requests(spa):
+    g = torch.Generator().manual_seed(4)
+    ctx, new = torch.randint(0, 40, (2000,), generator=g).tolist(), torch.randint(0, 3, (2000,), generator=g).tolist()
+    ctx[1500], new[1500], new[700] = 3000, 1, 60
+    step = oracle.Step(2000, ctx, new, q_heads=2, kv_heads=1, head_dim=64, page=16)
+    _attn_close(spa, step, new=60)
 
 
 def test_attn_of_many_requests(spa):

@@ -50,7 +50,7 @@ def _plan(lib, p, change=None, n_free=50):
     (dict(n_pages=0), -2), (dict(n_pages=2 ** 25, page_size=64), -2), (dict(max_pages=0), -2), (dict(max_pages=2 ** 24 + 1), -2),
     (dict(n_tokens=0), -2), (dict(n_tokens=2 ** 24 + 1), -2), (dict(n_tokens=2 ** 24, n_q_heads=256, n_kv_heads=2), -2), (dict(max_new_tokens=-1), -2),
     (dict(softmax_scale=-1.0), -2), (dict(softmax_scale=float("nan")), -2), (dict(softmax_scale=float("inf")), -2),
-    (dict(n_sink_tokens=-1), -3), (dict(window_tokens=-1), -3), (dict(softcap=-1.0), -3), (dict(softcap=float("nan")), -3), (dict(softcap=float("inf")), -3),
+    (dict(n_sink_tokens=-1), -3), (dict(window_tokens=-1), -3), (dict(softcap=-1.0), -3), (dict(softcap=float("nan")), -3), (dict(softcap=float("inf")), -3), (dict(softcap=65537.0), -3),
 ])
 def test_bad_params_are_refused_by_every_call(lib, kw, code):
     p = _params(**kw)
