@@ -76,15 +76,17 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v) {
 }
 // The kernel for many rows, up to 64 requests: of four lengths of a piece the one with the least time, by a model.  512 workgroups run
 // at once and take about 1.6 us a key tile: the longest piece, or the rounds of average ones, whichever is more; then the merge, 5 us and
-// 0.03 for each piece.  With 2^9 pieces always, or 2^10: chunk of 2048 tokens 3040 / 3105 us, mixed step 493 / 455.  Short calls want
-// more pieces (87 tokens over 800, 12 row tiles of 14 tiles: in pieces of 7 tiles 27 us, of 2 19), those whose row tiles fill the chip none.
+// 0.03 for each piece.  The lengths: no cut; as many pieces as run at once (each of the `tiles` row tiles and KV heads may end in a
+// short one); twice or four times as long, for short calls; or two rounds of pieces.  With 2^9 pieces always, or 2^10: chunk of
+// 2048 tokens 3040 / 3105 us, mixed step 493 / 455 (now 396); 180 tokens over 22000, 48 row tiles: in 528 pieces 130, in 480 98; 87 tokens over 800, 12 row tiles of 14 key tiles, in pieces of 7: 27 us, of 2: 19.
 // A row of 16 lanes tries one length.
-__device__ __forceinline__ int many_rows_piece(const PagedArgs& a, const PagedPart& part, int64_t work, int lane) {
+__device__ __forceinline__ int many_rows_piece(const PagedArgs& a, const PagedPart& part, int64_t work, int64_t tiles, int lane) {
     const int least = shortest_piece(work, part);
-    const int base = piece_within((work + 511) >> 9, part);
-    const int turn = lane >> 4;
-    int p = turn == 0 ? kWholeAxis : base < 8 ? base << (turn - 1) : turn == 1 ? base >> 1 : turn == 2 ? base : 2 * base;
+    auto pieces_of = [&](int64_t n) { return n > tiles ? piece_within((work + n - tiles - 1) / (n - tiles), part) : kWholeAxis; };
+    const int fit = pieces_of(512), turn = lane >> 4;
+    int p = turn == 0 ? kWholeAxis : turn == 1 ? fit : turn == 2 ? (fit < 8 ? 4 * fit : pieces_of(1024)) : 2 * fit;
     if (p < least) p = least;
+    if (p > kWholeAxis) p = kWholeAxis;
     uint32_t units = 0, cut = 0, longest = 0;
     for (int b0 = 0; b0 < a.B; b0 += 16) {
         const PagedShare s = share_at(a, part, request_at(a, b0 + (lane & 15)), p);
@@ -109,16 +111,18 @@ template <bool MANY>
 __device__ __forceinline__ int part_piece(const PagedArgs& a, const PagedPart& part, const Request& first, int lane) {
     if (part.n_slots == 0) return kWholeAxis;
     int64_t work = 0;
+    uint32_t tiles = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         const PagedShare s = share_at(a, part, b0 == 0 ? first : request_at(a, b0 + lane), kWholeAxis);
         work += (int64_t)s.tiles * s.keys;
+        tiles += (uint32_t)s.tiles;
     }
     // the lanes' sum in two halves of 24 bits; a lane's work of 2^48 and more makes the piece as long as any key axis either way
     const uint32_t lo = last_lane(wave_scan((uint32_t)(work & 0xffffff)));
     const uint32_t hi = last_lane(wave_scan((uint32_t)(work >> 24 > 0xffffff ? 0xffffff : work >> 24)));
     work = (((int64_t)hi << 24) + lo) * a.Hkv;
     if constexpr (!MANY) return few_rows_piece(work, part);
-    else return a.B <= 64 ? many_rows_piece(a, part, work, lane) : shortest_piece(work, part);
+    else return a.B <= 64 ? many_rows_piece(a, part, work, (int64_t)last_lane(wave_scan(tiles)) * a.Hkv, lane) : shortest_piece(work, part);
 }
 
 // What a workgroup of a part serves: unit `unit` of request b, counted from the longest row tiles, KV heads next to each
