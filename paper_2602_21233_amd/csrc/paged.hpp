@@ -22,7 +22,7 @@ struct PagedDims {
 struct PagedPart {
     int m, log_m, span;
     int log_most, min_tiles;
-    int whole_tiles;                  // tables of up to so many key tiles are not cut at all (no workspace, no merge)
+    int whole_tiles;                  // key axes of at most so many tiles are not cut (no workspace, no merge)
     int row_lo, row_hi;
     int n_slots;                      // partial results that the workspace has room for; 0: nothing is cut
     float *o, *lse;                   // partial results: [n_slots][m][D], [n_slots][m]; lse in base 2

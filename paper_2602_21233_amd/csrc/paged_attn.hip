@@ -78,7 +78,8 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v) {
 // at once and take about 1.6 us a key tile: the longest piece, or the rounds of average ones, whichever is more; then the merge, 5 us and
 // 0.03 for each piece.  The lengths: no cut; as many pieces as run at once (each of the `tiles` row tiles and KV heads may end in a
 // short one); twice or four times as long, for short calls; or two rounds of pieces.  With 2^9 pieces always, or 2^10: chunk of
-// 2048 tokens 3040 / 3105 us, mixed step 493 / 455 (now 396); 180 tokens over 22000, 48 row tiles: in 528 pieces 130, in 480 98; 87 tokens over 800, 12 row tiles of 14 key tiles, in pieces of 7: 27 us, of 2: 19.
+// 2048 tokens 3040 / 3105 us, mixed step 493 / 455 (now 396); 180 tokens over 22000, 48 row tiles, in 528 pieces: 130 us, in 480: 98;
+// 87 tokens over 800, 12 row tiles of 14 key tiles, in pieces of 7: 27 us, of 2: 19.
 // A row of 16 lanes tries one length.
 __device__ __forceinline__ int many_rows_piece(const PagedArgs& a, const PagedPart& part, int64_t work, int64_t tiles, int lane) {
     const int least = shortest_piece(work, part);
@@ -1098,19 +1099,21 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a, PagedPart
     if (many.n_slots > 0) merge_rows<D, NV, true>(a, many);
 }
 
+// Most key tiles of a row tile, by the table's width and the window.  Where they are few, the merge's 5 us are more than pieces save
+// (4 tokens behind 1498 keys, window 76: 13.8 -> 9.4 us; 39 behind 1183, window 3: 15.4 -> 11.1).
+int most_key_tiles_of(const PagedDims& d, const PagedPart& part) { return most_key_tiles(d.T, d.C << d.log_p, part.span, d.sink, d.window); }
 // Most workgroups of a part that a call can need, whatever its lengths (2^log_most more than without cuts, and none cut into pieces
 // of less than min_tiles)
-int64_t key_tiles_of_table(const PagedDims& d) { return (((int64_t)d.C << d.log_p) + kPagedTile - 1) / kPagedTile; }
 int64_t most_units(const PagedDims& d, const PagedPart& part) {
     const int64_t requests = d.B < d.T ? d.B : d.T;
     const int64_t tiles = (part.row_hi <= part.m ? requests : (int64_t)d.T * d.G / part.m + requests) * d.Hkv;
-    if (key_tiles_of_table(d) <= part.whole_tiles) return tiles;
-    const int64_t most = 1ll << part.log_most, cuts = (key_tiles_of_table(d) + part.min_tiles - 1) / part.min_tiles;
+    if (most_key_tiles_of(d, part) <= part.whole_tiles) return tiles;
+    const int64_t most = 1ll << part.log_most, cuts = (most_key_tiles_of(d, part) + part.min_tiles - 1) / part.min_tiles;
     return tiles * cuts < tiles + most ? tiles * cuts : tiles + most;
 }
 // Most partial results: requests that are cut have at most twice as many pieces as their work fills
 int64_t most_slots(const PagedDims& d, const PagedPart& part) {
-    if (key_tiles_of_table(d) <= part.whole_tiles) return 0;
+    if (most_key_tiles_of(d, part) <= part.whole_tiles) return 0;
     const int64_t units = most_units(d, part), most = 2ll << part.log_most;
     return units < most ? units : most;
 }

@@ -66,3 +66,16 @@ def test_pieces_stay_in_the_workspace(shim, log_most, min_tiles, few):
                 units += out[0] * out[2] * Hkv
                 slots += out[0] * out[2] * Hkv if out[2] > 1 else 0
             assert units <= 2 ** log_most + len(lens) * Hkv and slots <= 2 * 2 ** log_most
+
+
+@pytest.mark.parametrize("sink,window", [(0, 0), (0, 1), (5, 64), (64, 100), (300, 500), (0, 4096), (2 ** 30, 2 ** 30)])
+@pytest.mark.parametrize("m,G", [(16, 4), (32, 3), (128, 1), (128, 5), (128, 70)])
+def test_no_request_has_more_key_tiles_than_the_table_allows(shim, sink, window, m, G):
+    """What the host lays out from the table's width and all the tokens holds for each request's own lengths."""
+    span = (m + G - 1) // G + 1
+    for total, width in ((1, 64), (7, 16), (200, 1000), (4096, 8192), (2 ** 24, 2 ** 30)):
+        most = shim.most(total, width, span, sink, window)
+        for q_len in {1, 2, total // 2 or 1, total}:
+            for kv in {0, 1, 63, 64, width // 2, width - 1, width}:
+                if q_len <= total and kv <= width:
+                    assert shim.most(q_len, kv, span, sink, window) <= most
