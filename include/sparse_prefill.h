@@ -67,8 +67,8 @@ enum {
     SPA_ERR_LAUNCH = -6,              /* the HIP runtime rejected a launch                  */
     SPA_ERR_STATIC_SCRATCH_TOO_SMALL = -7, /* sparse_prefill_select_static: the call needs more than
                                          SPA_STATIC_SCRATCH_BYTES of scratch                 */
-    SPA_ERR_OVERLAP = -8              /* sparse_prefill_paged_plan: an array that is written
-                                         overlaps another one                                */
+    SPA_ERR_OVERLAP = -8              /* paged calls: an array that is written overlaps another
+                                         one                                                 */
 };
 
 typedef struct spa_params {
@@ -442,7 +442,8 @@ int sparse_prefill_paged_plan(const spa_paged_params *p, const int32_t *ctx_lens
 
 /* Keys and values of the new tokens into their pages: k, v [n_tokens, n_kv_heads, head_dim] (strides
  * k_stride, v_stride), token t to slots[t]; a slot outside the cache (-1 for padding) is passed over.  Every
- * other token of the cache keeps its bits.  A slot that occurs twice ends up with either token's values.
+ * other token of the cache keeps its bits.  A slot that occurs twice ends up with either token's values.  k and v
+ * may not lie in the cache, nor K and V pages on each other (SPA_ERR_OVERLAP where they are the same).
  * Uses of p: n_kv_heads, head_dim, page_size, n_pages, n_tokens, strides. */
 int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const void *v, const int32_t *slots,
                                 void *k_pages, void *vt_pages, void *hip_stream);
@@ -456,6 +457,7 @@ int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const 
  * sees no key (kv_lens[b] = 0, or a position below 0) gets zeros and -inf.  What lies behind a request's last key, and
  * what no query of the call sees, may be anything, NaN too; a key that a query does not see has no influence on it,
  * whatever its key and value are.  Infinite and NaN values that it sees reach it as arithmetic has it.
+ * out and lse may overlap nothing that the call reads: there is no attention in place (SPA_ERR_OVERLAP for out = q).
  * ws: spa_paged_workspace_bytes() bytes, 256-byte aligned; its contents need not survive between calls, calls
  * that overlap in time need one each. */
 int sparse_prefill_paged_attn(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,

@@ -102,6 +102,7 @@ int sparse_prefill_paged_append(const spa_paged_params* p, const void* k, const 
     const int64_t page = (int64_t)p->page_size * p->head_dim;
     if ((rc = check_strided(k, p->k_stride, 0)) || (rc = check_strided(v, p->v_stride, 0))) return rc;
     if ((rc = check_strided(k_pages, p->kp_stride, page)) || (rc = check_strided(vt_pages, p->vp_stride, page))) return rc;
+    if (k_pages == vt_pages) return SPA_ERR_OVERLAP;
     return launch_code(launch_paged_append(paged_dims(p), k, p->k_stride[0], p->k_stride[1], v, p->v_stride[0], p->v_stride[1], slots,
                                            k_pages, vt_pages, (hipStream_t)hip_stream));
 }
@@ -121,6 +122,7 @@ int sparse_prefill_paged_attn(const spa_paged_params* p, const void* q, const vo
     if (parts.ws_bytes > 0 && !ws) return SPA_ERR_NULLPTR;
     if (((uintptr_t)ws) & 255u) return SPA_ERR_BAD_STRIDE;
     if (ws_bytes < parts.ws_bytes) return SPA_ERR_WORKSPACE_TOO_SMALL;
+    if (out == q || k_pages == vt_pages) return SPA_ERR_OVERLAP;     // several workgroups read a query whose output one of them writes
     return launch_code(launch_paged_attn(d, parts, q, k_pages, vt_pages, block_table, q_starts, kv_lens, slopes_or_null, out, lse_or_null,
                                          (hipStream_t)hip_stream));
 }

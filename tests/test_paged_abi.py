@@ -133,3 +133,10 @@ def test_packed_params_equal_their_fields():
     p = _params(softmax_scale=0.25, n_sink_tokens=5, window_tokens=6, softcap=7.5, max_new_tokens=4)
     assert [getattr(p, n) for n, _ in binding.SpaPagedParams._fields_[:14]] == [3, 8, 2, 128, 64, 100, 20, 30, 4, 0.25, 5, 6, 7.5, 20]
     assert [tuple(getattr(p, n)) for n, _ in binding.SpaPagedParams._fields_[14:]] == [(1024, 128), (256, 128), (256, 128), (1024, 128), (16384, 8192), (16384, 8192)]
+
+
+def test_attention_in_place_and_one_tensor_for_k_and_v_pages_are_refused(lib):
+    p = _params()
+    assert _attn(lib, p, dict(out=FAKE, q=FAKE, k=FAKE + 0x1000, vt=FAKE + 0x2000)) == -8
+    assert _attn(lib, p, dict(out=FAKE + 0x1000, q=FAKE, k=FAKE + 0x2000, vt=FAKE + 0x2000)) == -8
+    assert _append(lib, p, dict(k_pages=FAKE + 0x1000, vt_pages=FAKE + 0x1000)) == -8
