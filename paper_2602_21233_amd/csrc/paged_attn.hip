@@ -7,9 +7,11 @@
 //
 // Softmax in base 2: x = (scaled logit) * log2 e, weights 2^(x - m) against a reference m that is set by the first tile and
 // moved only when a query's running denominator passes 2^40; the normalisation makes the result independent of m.  Logits,
-// weights' sums and outputs are held in fp32; the weights are rounded to bf16 for the second matrix product, whose other
-// operand is bf16 anyway: an error of at most 2^-8 of each term, about that of the bf16 output
-// (measured against 64 bits: 0.0019 to 0.0024 of the norm, 0.0017 of it from the output's rounding alone).
+// weights' sums and outputs are held in fp32.  The second matrix product takes weights in bf16.  The kernel for few rows waits for
+// the memory and gives it two bf16 parts of each, 16 bits in all: an error of 2^-16 of a term, lost in the output's rounding (against 64 bits
+// 0.0016 to 0.0017 of the norm, as from that rounding alone; 0.0019 to 0.0024 with one part; the same time).  The kernel for many rows
+// is bound by its matrix products, of which a second part would make half as many again, and rounds the weights to bf16 once, as the
+// sparse prefill does: 2^-8 of a term, about that of the bf16 output (0.0019 to 0.0023 of the norm in all).
 #include "attn_parts.hpp"
 #include "paged.hpp"
 
@@ -302,16 +304,16 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
         bf16x8 k0[DS], k1[DS];
         u32x4 v[DT];
     };
+    auto v_of = [&](int c, const Pages& pg) __attribute__((always_inline)) {       // a lane's 8 keys of dim dv0 + n16; other tiles 16 page further
+        const int in_page = SMALL ? 0 : key_of(c) & (page - 1);
+        const int id = SMALL && g >= 2 ? pg.id[SMALL ? 1 : 0] : pg.id[0];
+        return a.vt + id * a.vp_p + kvh * a.vp_h + in_page + 8 * (SMALL ? g & 1 : g) + (int64_t)(dv0 + n16) * page;
+    };
     auto load = [&](int c, const Pages& pg, Chunk& ch) __attribute__((always_inline)) {
-        const int key0 = key_of(c);
-        int id_k = pg.id[0], id_v = pg.id[0];
-        if constexpr (SMALL) {
-            if (n16 >= 8) id_k = pg.id[1];
-            if (g >= 2) id_v = pg.id[1];
-        }
-        const int in_page = SMALL ? 0 : key0 & (page - 1);
+        const int in_page = SMALL ? 0 : key_of(c) & (page - 1);
+        const int id_k = SMALL && n16 >= 8 ? pg.id[SMALL ? 1 : 0] : pg.id[0];
         const uint16_t* kp = a.k + id_k * a.kp_p + kvh * a.kp_h + (in_page + (SMALL ? k_row & 15 : k_row)) * D + 8 * g;
-        const uint16_t* vp = a.vt + id_v * a.vp_p + kvh * a.vp_h + in_page + 8 * (SMALL ? g & 1 : g) + (int64_t)(dv0 + n16) * page;
+        const uint16_t* vp = v_of(c, pg);
 #pragma unroll
         for (int s = 0; s < DS; ++s) {
             ch.k0[s] = *reinterpret_cast<const bf16x8*>(kp + 32 * s);
@@ -407,9 +409,13 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
             }
             l[f] += sum;
             const bf16x8 p = __builtin_convertvector(w, bf16x8);
+            const bf16x8 rest = __builtin_convertvector(w - __builtin_convertvector(p, f32x8), bf16x8);
 #pragma unroll
             for (int t = 0; t < DT; ++t)
                 o[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ch.v[t]), p, o[f][t], 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+                o[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ch.v[t]), rest, o[f][t], 0, 0, 0);
         }
     };
     int c = 2 * cut * per + wave;
@@ -423,28 +429,53 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
         }
     }
 
-    if (put_back) {                                             // rare: infinite and NaN values, for the rows that see them
-        for (int cc = 2 * cut * per + wave; cc < c_end; cc += NW) {
-            const int key0 = key_of(cc);
-            if (!hides(a, pos_lo, pos_hi, key0, 32)) continue;
-            for (int key = key0; key < key0 + 32 && key <= pos_hi; ++key) {
-                const uint16_t* const src = a.vt + page_of(key) * a.vp_p + kvh * a.vp_h + (int64_t)dv0 * page + (key & (page - 1));
-                int step = page;                                // unknown to the compiler, which would keep all the offsets in registers
-                asm volatile("" : "+s"(step));
+    // Infinite and NaN values, for the rows that see them: rare.  Those of masked chunks have been taken out, others have met a weight in two
+    // parts, the second of which may be 0 or negative.  What a row has of them in a dim is counted, by products of 0 and 1: those that make it
+    // +infinite or NaN, and -infinite or NaN.  Finite terms do not matter where there is one.
+    bool left = put_back;
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) left |= !(fabsf(o[f][t][r]) < INFINITY);
+    if (__any(left)) {
+#pragma unroll 1
+        for (int tt = 0; tt < DT; ++tt) {
+            f32x4 up[MF], down[MF];
+#pragma unroll
+            for (int f = 0; f < MF; ++f) up[f] = down[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int cc = 2 * cut * per + wave; cc < c_end; cc += NW) {
+                const u32x4 v = *reinterpret_cast<const u32x4*>(v_of(cc, pages_of(cc)) + 16 * tt * page);
+                u32x4 ups = {0u, 0u, 0u, 0u}, downs = ups;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const uint32_t u = v[x >> 1] >> (16 * (x & 1)) & 0xffffu, one = 0x3f80u << (16 * (x & 1));
+                    const bool nan = (u & 0x7fffu) > 0x7f80u;
+                    ups[x >> 1] |= nan || u == 0x7f80u ? one : 0u;
+                    downs[x >> 1] |= nan || u == 0xff80u ? one : 0u;
+                }
+                if (!__any((ups[0] | ups[1] | ups[2] | ups[3] | downs[0] | downs[1] | downs[2] | downs[3]) != 0)) continue;
 #pragma unroll
                 for (int f = 0; f < MF; ++f) {
-                    if (!sees(a, pos[f], key)) continue;
+                    f32x8 seen;
 #pragma unroll
-                    for (int t = 0; t < DT; ++t) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const uint32_t u = src[(16 * t + 4 * g + r) * step];
-                            if (not_finite(u)) o[f][t][r] += __uint_as_float(u << 16);
-                        }
-                        asm volatile("" ::: "memory");           // four loads at a time: the registers are for the usual case
-                    }
+                    for (int r = 0; r < 8; ++r) seen[r] = sees(a, pos[f], key_of(cc) + 8 * g + r) ? 1.f : 0.f;
+                    const bf16x8 s = __builtin_convertvector(seen, bf16x8);
+                    up[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ups), s, up[f], 0, 0, 0);
+                    down[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, downs), s, down[f], 0, 0, 0);
                 }
             }
+#pragma unroll
+            for (int f = 0; f < MF; ++f)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float value = up[f][r] > 0.f ? (down[f][r] > 0.f ? NAN : INFINITY) : -INFINITY;
+                    const bool some = up[f][r] + down[f][r] > 0.f;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) o[f][t][r] = some && t == tt ? value : o[f][t][r];
+                }
         }
     }
 

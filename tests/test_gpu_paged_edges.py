@@ -1,0 +1,73 @@
+"""Edges of the paged KV cache on the GPU: how exact a few rows' attention is, values that are not finite, calls that are cut, lists of
+slots long enough for the append kernel of prompts, malformed lengths next to memory that must not change.  Against the plain 64-bit forms
+of tests/paged_oracle.py."""
+import math
+
+import pytest
+import torch
+
+import paged_oracle as oracle
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def spa():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2602_21233_amd as m
+    m.load_library()
+    return m
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _attn(spa, step, **how):
+    return spa.paged_attn(step.q.cuda(), step.k_pages.cuda(), step.vt_pages.cuda(), step.table.cuda(), _i32(step.starts), _i32(step.kv_lens), **how)
+
+
+# ------------------------------------------------------------------------------------- weights of few rows keep 16 bits
+def _within_the_output_s_rounding(step, out, rows):
+    """The oracle's tolerance with another share for the weights: two bf16 parts leave a rest of 2^-8 of 2^-8 of a weight, and the sum of
+    n products in fp32 takes at most 2^-23 of their sizes a term (half a step, or a whole one where the matrix unit cuts off)."""
+    want, _, tol, _ = step.want()
+    mass = oracle.attn(step.q, step.keys, [v.abs() for v in step.values], step.starts, step.kv_lens)[0]
+    n = max(step.kv_lens)
+    tol = tol - 1.01 * 2 ** -8 * mass + (1.01 * 2 ** -16 + (n + 8) * 2 ** -23) * mass
+    off = (out.cpu().double() - want).abs() - tol
+    assert off[rows].max().item() <= 0, (off[rows].max().item(), (off == off[rows].max()).nonzero()[0].tolist())
+
+
+@pytest.mark.parametrize("head_dim,page,q_heads,kv_heads", [(128, 64, 4, 1), (64, 16, 8, 2), (128, 16, 16, 1), (128, 32, 20, 1), (64, 128, 32, 1)])
+@pytest.mark.parametrize("batch", [1, 5, 90])
+def test_single_tokens_are_as_exact_as_the_output_type(spa, batch, head_dim, page, q_heads, kv_heads):
+    """Few and many requests, 16 and 32 rows a workgroup: every kernel for few rows."""
+    g = torch.Generator().manual_seed(batch)
+    ctx = torch.randint(0, 120, (batch,), generator=g).tolist()
+    step = oracle.Step(batch + page, ctx, [1] * batch, page=page, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim)
+    _within_the_output_s_rounding(step, _attn(spa, step, max_new_tokens=1), slice(None))
+
+
+def test_single_tokens_next_to_a_chunk_are_as_exact_as_the_output_type(spa):
+    step = oracle.Step(7, [60, 40, 3, 100], [1, 2, 70, 4], q_heads=4, kv_heads=1)
+    rows = [t for b in (0, 1, 3) for t in range(step.starts[b], step.starts[b + 1])]
+    _within_the_output_s_rounding(step, _attn(spa, step, max_new_tokens=70), rows)
+
+
+def test_cut_key_axes_are_as_exact_as_the_output_type(spa):
+    """700 keys in pieces of four tiles and their merge."""
+    step = oracle.Step(8, [700], [1], q_heads=4, kv_heads=1)
+    _within_the_output_s_rounding(step, _attn(spa, step, max_new_tokens=1), slice(None))
+
+
+@pytest.mark.parametrize("q_heads", [4, 20])
+def test_infinite_values_with_weights_of_one_part(spa, q_heads):
+    """A weight of 1 has nothing left for its second part: 0 times an infinite value must not show."""
+    step = oracle.Step(1, [0, 0, 0, 0], [1, 1, 1, 1], q_heads=q_heads, kv_heads=1, head_dim=64)
+    for b, value in enumerate((math.inf, -math.inf, math.nan)):
+        step.vt_pages[step.table[b, 0], 0, 5, 0] = value
+    got, values = _attn(spa, step).float().cpu(), torch.stack([v[0, 0] for v in step.values]).float()
+    values[:3, 5] = torch.tensor([math.inf, -math.inf, math.nan])
+    assert torch.equal(got.nan_to_num(7e9), values[:, None].expand_as(got).nan_to_num(7e9))
