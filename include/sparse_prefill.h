@@ -457,7 +457,8 @@ int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const 
  * on the device (bias by distance).  lse_or_null: [n_tokens, n_q_heads] fp32, ln sum_j e^x_j.  A query that
  * sees no key (kv_lens[b] = 0, or a position below 0) gets zeros and -inf.  What lies behind a request's last key, and
  * what no query of the call sees, may be anything, NaN too; a key that a query does not see has no influence on it,
- * whatever its key and value are.  Infinite and NaN values that it sees reach it as arithmetic has it.
+ * whatever its key and value are.  A NaN value that a query sees makes its output NaN in that dim, an infinite one infinite, or NaN where
+ * infinities of both signs meet or its weight is too small for fp32; however the call is cut.
  * out and lse may overlap nothing that the call reads: there is no attention in place (SPA_ERR_OVERLAP for out = q).
  * ws: spa_paged_workspace_bytes() bytes, 256-byte aligned; its contents need not survive between calls, calls
  * that overlap in time need one each. */

@@ -1089,24 +1089,26 @@ __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& 
             const float old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - mx_new);
             mx = mx_new;
             const float w = v == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(v - mx);
+            const uint64_t with_keys = __ballot(v != -INFINITY);    // of weight 0, too: the piece may hold an infinite or NaN value
             total = fmaf(total, old, w);
             acc *= old;
             const int n = min(64, splits - s0);
             for (int s = 0; s < n; s += 4 * NG) {           // four loads of a lane in flight
                 float ws[4];
+                bool some[4];
                 f32x4 p[4];
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                     const int mine = s + NG * y + grp, there = min(mine, n - 1);
-                    const float wy = __shfl(w, there);
-                    ws[y] = mine < n ? wy : 0.f;
+                    ws[y] = __shfl(w, there);
+                    some[y] = mine < n && (with_keys >> there & 1) != 0;
                     p[y] = *reinterpret_cast<const f32x4*>(part.o + at(s0 + there) * D + d0);
                 }
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
 #pragma unroll
                     for (int x = 0; x < 4; ++x)             // a piece without a key in sight may not have written its values
-                        acc[x] = ws[y] != 0.f ? fmaf(p[y][x], ws[y], acc[x]) : acc[x];
+                        acc[x] = some[y] ? fmaf(p[y][x], ws[y], acc[x]) : acc[x];
             }
         }
 #pragma unroll

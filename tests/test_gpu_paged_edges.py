@@ -71,3 +71,19 @@ def test_infinite_values_with_weights_of_one_part(spa, q_heads):
     got, values = _attn(spa, step).float().cpu(), torch.stack([v[0, 0] for v in step.values]).float()
     values[:3, 5] = torch.tensor([math.inf, -math.inf, math.nan])
     assert torch.equal(got.nan_to_num(7e9), values[:, None].expand_as(got).nan_to_num(7e9))
+
+
+# ------------------------------------------------------------------------------------------- pieces of a cut key axis
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_values_that_are_not_finite_in_a_piece_without_weight(spa, value, new):
+    """The bias leaves the first keys' piece a weight of 2^-2000 of the last one's, nothing in fp32."""
+    step = oracle.Step(3, [3000], [new], q_heads=4, kv_heads=1, head_dim=64)
+    slopes = torch.full((4,), 0.5, device="cuda")
+    clean = _attn(spa, step, max_new_tokens=new, slopes=slopes).float().cpu()
+    step.vt_pages[step.table[0, 0], 0, 7, 5] = value
+    got = _attn(spa, step, max_new_tokens=new, slopes=slopes).float().cpu()
+    odd = got[:, :, 7]
+    assert (torch.isnan(odd) | (odd == value)).all()
+    got[:, :, 7] = clean[:, :, 7]
+    assert torch.equal(got, clean)
