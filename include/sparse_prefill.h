@@ -455,7 +455,7 @@ int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const 
  * in fp32 with bf16 matrix products; out [n_tokens, n_q_heads, head_dim] bf16.  Softmax weights enter the second product rounded to 16
  * bits for requests of few rows (new tokens * query heads of a KV head: up to 16 at least), to bf16 for others.  slopes_or_null: n_q_heads fp32
  * on the device (bias by distance).  lse_or_null: [n_tokens, n_q_heads] fp32, ln sum_j e^x_j.  A query that
- * sees no key (kv_lens[b] = 0, or a position below 0) gets zeros and -inf.  What lies behind a request's last key, and
+ * sees no key (kv_lens[b] = 0, or a position below 0) gets zeros and -inf, one that only sees keys with logits of -inf NaN and -inf.  What lies behind a request's last key, and
  * what no query of the call sees, may be anything, NaN too; a key that a query does not see has no influence on it,
  * whatever its key and value are.  A NaN value that a query sees makes its output NaN in that dim, an infinite one infinite, or NaN where
  * infinities of both signs meet or its weight is too small for fp32; however the call is cut.

@@ -20,6 +20,11 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kRescaleAt = 1.099511627776e12f;      // 2^40
+// Base-2 log-sum-exp of a piece whose keys, if a row sees any, all have a logit of -infinity; -infinity itself where a piece has written no
+// values.  A row whose pieces all have it, or that has no pieces and found no finite logit, comes from a query that sees no key if its
+// position is below 0 (every other one sees its own key): zeros then, NaN otherwise, as 0 / 0 has it.
+constexpr float kNoLogit = -0x1.fffffep127f;      // the lowest finite value
+__device__ __forceinline__ float without_logits(int pos) { return pos < 0 ? 0.f : NAN; }
 
 struct PagedArgs {
     const uint16_t *q, *k, *vt;
@@ -512,9 +517,9 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
 #pragma unroll
                 for (int x = 0; x < VPT; ++x) acc[x] = fmaf(s_o[w][r16][d0 + x], scale, acc[x]);
             }
-            const bool none = mx == -INFINITY && lsum == 0.f;    // a row that sees no key (of this piece); NaN is not none
-            const float inv = none ? 0.f : 1.f / lsum;
-            const float lse2 = none ? -INFINITY : mx + __log2f(lsum);
+            const bool none = mx == -INFINITY && lsum == 0.f;    // no finite logit (in this piece); NaN is not none
+            const float inv = none ? (partial ? 0.f : without_logits(pos0 + row / a.G)) : 1.f / lsum;
+            const float lse2 = none ? (partial ? kNoLogit : -INFINITY) : mx + __log2f(lsum);
             if (partial) {
                 float* po = part.o + ((int64_t)slot * part.m + 16 * f + r16) * D + dv0 + d0;
 #pragma unroll
@@ -1024,9 +1029,9 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     }
 
     const float lt = l + other_half(l);
-    const bool none = l == INFINITY;         // a row that sees no key; NaN is not none
-    const float inv = none ? 0.f : 1.f / lt;
-    const float lse2 = none ? -INFINITY : m + __log2f(lt);
+    const bool none = l == INFINITY;         // no finite logit (in this piece); NaN is not none
+    const float inv = none ? (partial ? 0.f : without_logits(pos)) : 1.f / lt;
+    const float lse2 = none ? (partial ? kNoLogit : -INFINITY) : m + __log2f(lt);
     int at = 32 * wave + l32;
     asm volatile("" : "+v"(at));                           // found anew, not kept in registers all the way
     if (row0 + at > last_row) return;
@@ -1117,8 +1122,8 @@ __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& 
         for (int x = LPR; x < 64; x <<= 1)
 #pragma unroll
             for (int y = 0; y < 4; ++y) acc[y] += __shfl_xor(acc[y], x);
-        const bool none = total == 0.f;
-        const float inv = none ? 0.f : 1.f / total;
+        const bool none = total == 0.f || (mx <= kNoLogit && total == total);       // NaN is not none
+        const float inv = none ? without_logits(sh.r.kv - sh.r.len + row / a.G) : 1.f / total;
         if (lane < LPR) {
             const int tok = sh.r.first + row / a.G, hd = kvh * a.G + row % a.G;
             *reinterpret_cast<bf16x4*>(a.out + (int64_t)tok * a.o_t + hd * a.o_h + d0) = __builtin_convertvector(acc * inv, bf16x4);

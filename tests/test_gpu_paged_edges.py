@@ -87,3 +87,22 @@ def test_values_that_are_not_finite_in_a_piece_without_weight(spa, value, new):
     assert (torch.isnan(odd) | (odd == value)).all()
     got[:, :, 7] = clean[:, :, 7]
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("ctx,new", [(100, 1), (100, 40), (3000, 1), (3000, 40)])
+def test_keys_with_logits_of_minus_infinity(spa, ctx, new):
+    """Weights of 0 next to other keys, also where a whole piece has them; where a query sees no other key its output is NaN, and still zeros
+    where it sees none at all."""
+    step = oracle.Step(5, [ctx, ctx], [new, new], q_heads=4, kv_heads=1, head_dim=64)
+    step.q[:, :, 0] = 1.0
+    for b, upto in ((0, step.kv_lens[0] // 2), (1, step.kv_lens[1])):
+        step.keys[b][:, :upto, 0] = -math.inf
+        for key in range(upto):
+            step.k_pages[step.table[b, key // step.page], 0, key % step.page, 0] = -math.inf
+    out, lse = _attn(spa, step, max_new_tokens=new, return_lse=True)
+    want, want_lse, tol, lse_tol = oracle.attn(step.q[:new], step.keys[:1], step.values[:1], [0, new], step.kv_lens[:1])
+    assert ((out[:new].cpu().double() - want).abs() <= tol).all() and ((lse[:new].cpu().double() - want_lse).abs() <= lse_tol).all()
+    assert torch.isnan(out[new:]).all() and (lse[new:] == -math.inf).all()
+    step.kv_lens[1] = new - 1                                       # the first new token has no position
+    out, lse = _attn(spa, step, max_new_tokens=new, return_lse=True)
+    assert (out[new] == 0).all() and torch.isnan(out[new + 1:]).all() and (lse[new:] == -math.inf).all()
