@@ -388,7 +388,10 @@ int sparse_prefill_fused_ex(const spa_params *p, const void *q, const void *k, c
  *             tokens has position kv_lens[b] - n + i.
  * Lengths and tables are read on the device: no call needs them on the host, and a captured graph may
  * be replayed with others.  A malformed one (a page outside the cache, a length past max_pages, starts
- * that are not ascending) cannot make a kernel leave the tensors; the rows concerned are unspecified. */
+ * that are not ascending) cannot make a kernel leave the tensors; the rows concerned are unspecified.
+ * An array that a call writes (workspace among them) may lie neither on another one nor on itself: SPA_ERR_OVERLAP.  Of two arrays with strides
+ * rows between those of the other are fine where both have the same strides (slices of one tensor) or one is a single row; otherwise
+ * their extents must not meet. */
 typedef struct spa_paged_params {
     int32_t batch;          /* 1 .. 4096 requests                                               */
     int32_t n_q_heads;      /* >= 1, multiple of n_kv_heads                                     */
@@ -433,7 +436,7 @@ int spa_paged_workspace_bytes(const spa_paged_params *p, size_t *bytes);
  *   positions_or_null [n_tokens]: position of every new token in its request, 0 for padding
  *   taken     [2]: pages taken from the free list, requests left out
  * free_pages: n_free >= 0 int32 (NULL if there are none); free_range: 2 int32 on the device, clamped to
- * [0, n_free].  No array that is written may overlap another one.
+ * [0, n_free].
  * Uses of p: batch, page_size, n_pages, max_pages, n_tokens, table_stride. */
 int sparse_prefill_paged_plan(const spa_paged_params *p, const int32_t *ctx_lens, const int32_t *new_lens,
                               const int32_t *free_pages, int32_t n_free, const int32_t *free_range,
@@ -443,7 +446,7 @@ int sparse_prefill_paged_plan(const spa_paged_params *p, const int32_t *ctx_lens
 /* Keys and values of the new tokens into their pages: k, v [n_tokens, n_kv_heads, head_dim] (strides
  * k_stride, v_stride), token t to slots[t]; a slot outside the cache (-1 for padding) is passed over.  Every
  * other token of the cache keeps its bits.  A slot that occurs twice ends up with either token's values.  k and v
- * may not lie in the cache, nor K and V pages on each other (SPA_ERR_OVERLAP where they are the same).
+ * may not lie in the cache, nor K and V pages on each other.
  * Uses of p: n_kv_heads, head_dim, page_size, n_pages, n_tokens, strides. */
 int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const void *v, const int32_t *slots,
                                 void *k_pages, void *vt_pages, void *hip_stream);
@@ -459,7 +462,7 @@ int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const 
  * what no query of the call sees, may be anything, NaN too; a key that a query does not see has no influence on it,
  * whatever its key and value are.  A NaN value that a query sees makes its output NaN in that dim, an infinite one infinite, or NaN where
  * infinities of both signs meet or its weight is too small for fp32; however the call is cut.
- * out and lse may overlap nothing that the call reads: there is no attention in place (SPA_ERR_OVERLAP for out = q).
+ * There is no attention in place: out may not lie on q.
  * ws: spa_paged_workspace_bytes() bytes, 256-byte aligned; its contents need not survive between calls, calls
  * that overlap in time need one each. */
 int sparse_prefill_paged_attn(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,

@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparse_prefill.so")
 SOURCES = ("api.hip", "pool.hip", "select.hip", "select_d128.hip", "select_d64.hip", "attn.hip",
            "paged_api.hip", "paged_cache.hip", "paged_attn.hip")
-HEADERS = ("attn_parts.hpp", "common.hpp", "paged.hpp", "row_deal.hpp", "score_rows.hpp", "select_impl.hpp", "value_block.hpp", os.path.join("..", "..", "include", "sparse_prefill.h"))
+HEADERS = ("attn_parts.hpp", "common.hpp", "overlap.hpp", "paged.hpp", "row_deal.hpp", "score_rows.hpp", "select_impl.hpp", "value_block.hpp", os.path.join("..", "..", "include", "sparse_prefill.h"))
 
 # The attention kernel never produces NaN from finite inputs; telling the compiler so
 # removes the NaN-quieting v_max x,x pairs it otherwise puts around every fmaxf.

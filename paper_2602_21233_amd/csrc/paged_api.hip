@@ -2,6 +2,7 @@
 // Nothing here allocates, frees or synchronises; see include/sparse_prefill.h.
 #include <math.h>
 
+#include "overlap.hpp"
 #include "paged.hpp"
 
 using namespace spa;
@@ -51,11 +52,25 @@ PagedDims paged_dims(const spa_paged_params* p) {
     return d;
 }
 
-struct Range {
-    uintptr_t lo, hi;
-};
-Range range_of(const void* ptr, int64_t n) { return {(uintptr_t)ptr, (uintptr_t)ptr + (ptr ? 4 * (uintptr_t)n : 0)}; }
-bool overlap(const Range& a, const Range& b) { return a.lo < b.hi && b.lo < a.hi; }
+// arrays of a call as rows of bytes
+Rows words_of(const void* ptr, int64_t n) { return row_of(ptr, 4 * n); }
+Rows table_rows(const spa_paged_params* p, const int32_t* table) { return rows_of(table, p->batch, 4 * (wide)p->table_stride, 1, 0, 4ll * p->max_pages); }
+Rows token_rows(const spa_paged_params* p, const void* x, const int64_t s[2], int heads) { return rows_of(x, p->n_tokens, 2 * (wide)s[0], heads, 2 * (wide)s[1], 2ll * p->head_dim); }
+Rows page_rows(const spa_paged_params* p, const void* x, const int64_t s[2]) {
+    return rows_of(x, p->n_pages, 2 * (wide)s[0], p->n_kv_heads, 2 * (wide)s[1], 2ll * p->page_size * p->head_dim);
+}
+// whether a written array lies on a read one, on another written one or on itself
+template <int W, int R>
+bool clash(const Rows (&written)[W], const Rows (&read)[R]) {
+    for (int i = 0; i < W; ++i) {
+        if (overlaps_itself(written[i])) return true;
+        for (const Rows& r : read)
+            if (overlap(written[i], r)) return true;
+        for (int j = 0; j < i; ++j)
+            if (overlap(written[i], written[j])) return true;
+    }
+    return false;
+}
 
 int launch_code(hipError_t e) { return e == hipSuccess ? SPA_OK : SPA_ERR_LAUNCH; }
 
@@ -81,15 +96,10 @@ int sparse_prefill_paged_plan(const spa_paged_params* p, const int32_t* ctx_lens
     if (n_free < 0) return SPA_ERR_BAD_SHAPE;
     if (n_free > 0 && !free_pages) return SPA_ERR_NULLPTR;
     if ((rc = check_table(p))) return rc;
-    const Range read[] = {range_of(ctx_lens, p->batch), range_of(new_lens, p->batch), range_of(free_pages, n_free), range_of(free_range, 2)};
-    const Range written[] = {range_of(block_table, (int64_t)(p->batch - 1) * p->table_stride + p->max_pages), range_of(q_starts, p->batch + 1),
-                             range_of(kv_lens, p->batch), range_of(slots, p->n_tokens), range_of(positions_or_null, p->n_tokens), range_of(taken, 2)};
-    for (int i = 0; i < 6; ++i) {
-        for (const Range& r : read)
-            if (overlap(written[i], r)) return SPA_ERR_OVERLAP;
-        for (int j = 0; j < i; ++j)
-            if (overlap(written[i], written[j])) return SPA_ERR_OVERLAP;
-    }
+    const Rows read[] = {words_of(ctx_lens, p->batch), words_of(new_lens, p->batch), words_of(free_pages, n_free), words_of(free_range, 2)};
+    const Rows written[] = {table_rows(p, block_table), words_of(q_starts, p->batch + 1), words_of(kv_lens, p->batch), words_of(slots, p->n_tokens),
+                            words_of(positions_or_null, p->n_tokens), words_of(taken, 2)};
+    if (clash(written, read)) return SPA_ERR_OVERLAP;
     return launch_code(launch_paged_plan(paged_dims(p), ctx_lens, new_lens, free_pages, n_free, free_range, block_table, q_starts, kv_lens,
                                          slots, positions_or_null, taken, (hipStream_t)hip_stream));
 }
@@ -102,7 +112,9 @@ int sparse_prefill_paged_append(const spa_paged_params* p, const void* k, const 
     const int64_t page = (int64_t)p->page_size * p->head_dim;
     if ((rc = check_strided(k, p->k_stride, 0)) || (rc = check_strided(v, p->v_stride, 0))) return rc;
     if ((rc = check_strided(k_pages, p->kp_stride, page)) || (rc = check_strided(vt_pages, p->vp_stride, page))) return rc;
-    if (k_pages == vt_pages) return SPA_ERR_OVERLAP;
+    const Rows read[] = {token_rows(p, k, p->k_stride, p->n_kv_heads), token_rows(p, v, p->v_stride, p->n_kv_heads), words_of(slots, p->n_tokens)};
+    const Rows written[] = {page_rows(p, k_pages, p->kp_stride), page_rows(p, vt_pages, p->vp_stride)};
+    if (clash(written, read)) return SPA_ERR_OVERLAP;
     return launch_code(launch_paged_append(paged_dims(p), k, p->k_stride[0], p->k_stride[1], v, p->v_stride[0], p->v_stride[1], slots,
                                            k_pages, vt_pages, (hipStream_t)hip_stream));
 }
@@ -122,7 +134,12 @@ int sparse_prefill_paged_attn(const spa_paged_params* p, const void* q, const vo
     if (parts.ws_bytes > 0 && !ws) return SPA_ERR_NULLPTR;
     if (((uintptr_t)ws) & 255u) return SPA_ERR_BAD_STRIDE;
     if (ws_bytes < parts.ws_bytes) return SPA_ERR_WORKSPACE_TOO_SMALL;
-    if (out == q || k_pages == vt_pages) return SPA_ERR_OVERLAP;     // several workgroups read a query whose output one of them writes
+    // several workgroups read a query whose output one of them writes
+    const Rows read[] = {token_rows(p, q, p->q_stride, p->n_q_heads), page_rows(p, k_pages, p->kp_stride), page_rows(p, vt_pages, p->vp_stride),
+                         table_rows(p, block_table), words_of(q_starts, p->batch + 1), words_of(kv_lens, p->batch), words_of(slopes_or_null, p->n_q_heads)};
+    const Rows written[] = {token_rows(p, out, p->o_stride, p->n_q_heads), words_of(lse_or_null, (int64_t)p->n_tokens * p->n_q_heads),
+                            row_of(ws, (int64_t)parts.ws_bytes)};
+    if (clash(written, read) || k_pages == vt_pages) return SPA_ERR_OVERLAP;
     return launch_code(launch_paged_attn(d, parts, q, k_pages, vt_pages, block_table, q_starts, kv_lens, slopes_or_null, out, lse_or_null,
                                          (hipStream_t)hip_stream));
 }

@@ -106,3 +106,20 @@ def test_keys_with_logits_of_minus_infinity(spa, ctx, new):
     step.kv_lens[1] = new - 1                                       # the first new token has no position
     out, lse = _attn(spa, step, max_new_tokens=new, return_lse=True)
     assert (out[new] == 0).all() and torch.isnan(out[new + 1:]).all() and (lse[new:] == -math.inf).all()
+
+
+# ------------------------------------------------------------------------------------------------ arrays in one tensor
+def test_queries_and_outputs_as_slices_of_one_tensor(spa):
+    """out in the place of the keys that the step has appended, next to its own queries; on them it is refused."""
+    step = oracle.Step(6, [90, 10, 400], [1, 40, 2], q_heads=4, kv_heads=2, head_dim=64)
+    qkv = torch.full((step.T, 12, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    qkv[:, :4] = step.q.cuda()
+    t = step.k_pages.cuda(), step.vt_pages.cuda(), step.table.cuda(), _i32(step.starts), _i32(step.kv_lens)
+    want = spa.paged_attn(step.q.cuda(), *t)
+    got = spa.paged_attn(qkv[:, :4], *t, out=qkv[:, 4:8])
+    assert torch.equal(got, want) and torch.equal(qkv[:, 4:8], want) and (qkv[:, 8:] == 7.0).all() and torch.equal(qkv[:, :4].cpu(), step.q)
+    for h in (0, 1, 3):
+        with pytest.raises(spa.SpaError):
+            spa.paged_attn(qkv[:, :4], *t, out=qkv[:, h:h + 4])
+    with pytest.raises(spa.SpaError):
+        spa.paged_attn(qkv[1:, :4], *t, out=qkv[:-1, :4])
