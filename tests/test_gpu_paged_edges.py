@@ -123,3 +123,84 @@ def test_queries_and_outputs_as_slices_of_one_tensor(spa):
             spa.paged_attn(qkv[:, :4], *t, out=qkv[:, h:h + 4])
     with pytest.raises(spa.SpaError):
         spa.paged_attn(qkv[1:, :4], *t, out=qkv[:-1, :4])
+
+
+# --------------------------------------------------------------------------- append: the kernel for more than 1024 tokens
+def _bits(*shape, seed=0):
+    """bf16 values of any bits, NaN payloads among them"""
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(-2 ** 15, 2 ** 15, shape, generator=g).to(torch.int16).view(torch.bfloat16)
+
+
+def _same_bits(a, b):
+    return torch.equal(a.cpu().view(torch.int16), b.cpu().view(torch.int16))
+
+
+def _prompts(T, n_pages, page, seed):
+    """Slots of prompts whose first and last tokens lie inside pages, the pages in any order; padding behind them."""
+    g = torch.Generator().manual_seed(seed)
+    draw = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=g))  # noqa: E731
+    ids, slots = torch.randperm(n_pages, generator=g).tolist(), []
+    while len(slots) < T:
+        ctx, n = draw(0, 2 * page), min(draw(1, 500), T - len(slots))
+        pages = [ids.pop() for _ in range(-(-(ctx % page + n) // page))]
+        slots += [pages[(ctx % page + i) // page] * page + (ctx % page + i) % page for i in range(n)]
+        if len(slots) < T and draw(0, 3) == 0:
+            slots.append(-1)
+    return slots
+
+
+def _long_slot_maps(T, n_pages, page):
+    n = n_pages * page
+    yield "scattered", torch.randperm(n, generator=torch.Generator().manual_seed(T)).tolist()[:T]
+    for start in (0, 1, 4, 7):                                     # a piece begins at token 0, 7, 4, 1 and every 8th from there, over the borders of 64
+        yield f"one run from {start}", list(range(start, start + T))
+    yield "prompts", _prompts(T, n_pages, page, T)
+    yield "gaps", [s if (s + 3) % 13 else -1 for s in range(2, T + 2)]
+    yield "backwards", list(range(T - 1, -1, -1))
+    yield "wild", [(n + s, -1 - s, 2 ** 31 - 1 - s, s)[s % 4] if s % 64 > 50 else s for s in range(T)]
+    yield "swapped pairs", [s ^ 1 for s in range(T + 1)][:T]
+
+
+@pytest.mark.parametrize("T", [1024, 1025, 1087, 3101])
+@pytest.mark.parametrize("head_dim,page,heads", [(64, 16, 3), (128, 32, 1), (128, 64, 2), (64, 128, 1)])
+def test_append_of_many_tokens_moves_the_bits(spa, head_dim, page, heads, T):
+    n_pages = 2 * T // page + 40
+    k_pages, vt_pages = _bits(n_pages, heads, page, head_dim, seed=90), _bits(n_pages, heads, head_dim, page, seed=91)
+    for turn, (name, slots) in enumerate(_long_slot_maps(T, n_pages, page)):
+        k, v = _bits(T, heads, head_dim, seed=turn), _bits(T, heads, head_dim, seed=50 + turn)
+        want = oracle.append(k, v, torch.tensor(slots), k_pages, vt_pages)
+        mine = k_pages.cuda(), vt_pages.cuda()
+        spa.paged_append(k.cuda(), v.cuda(), _i32(slots), *mine)
+        assert _same_bits(mine[0], want[0]) and _same_bits(mine[1], want[1]), name
+
+
+def test_append_of_many_strided_tokens(spa):
+    """K and V out of one projection's output and out of [heads, tokens, dim]; pages of both in one allocation, with room between them."""
+    T, H, D, page, N = 1500, 3, 128, 32, 60
+    qkv, v = _bits(T, 4 * H, D + 8, seed=1).cuda(), _bits(H, T, D, seed=2).cuda().transpose(0, 1)
+    both = _bits(N, 5, H, page * D, seed=3).cuda()
+    before = both.clone()
+    k_pages, vt_pages = both[:, 1].view(N, H, page, D), both[:, 3].view(N, H, D, page)
+    slots = _prompts(T, N, page, 9)
+    want = oracle.append(qkv[:, H:2 * H, :D].cpu(), v.cpu(), torch.tensor(slots), k_pages.cpu(), vt_pages.cpu())
+    spa.paged_append(qkv[:, H:2 * H, :D], v, _i32(slots), k_pages, vt_pages)
+    assert _same_bits(k_pages, want[0]) and _same_bits(vt_pages, want[1])
+    assert all(_same_bits(both[:, i], before[:, i]) for i in (0, 2, 4))
+
+
+def test_append_of_many_tokens_far_past_32_bit_offsets(spa):
+    page, H, D, T = 128, 1, 128, 1300
+    n_pages = 5 * 2 ** 30 // (page * H * D * 2)
+    k_pages = torch.zeros((n_pages, H, page, D), dtype=torch.bfloat16, device="cuda")
+    vt_pages = torch.zeros((n_pages, H, D, page), dtype=torch.bfloat16, device="cuda")
+    k, v = _bits(T, H, D, seed=1), _bits(T, H, D, seed=2)
+    first = n_pages * page - T - 3                                  # up to the third last slot of the cache
+    spa.paged_append(k.cuda(), v.cuda(), _i32(list(range(first, first + T))), k_pages, vt_pages)
+    at = first // page
+    got_k = k_pages[at:].transpose(1, 2).reshape(-1, H, D)
+    got_v = vt_pages[at:].permute(0, 3, 1, 2).reshape(-1, H, D)
+    skip = first - at * page
+    for got, x in ((got_k, k), (got_v, v)):
+        assert _same_bits(got[skip:skip + T], x) and (got[:skip] == 0).all() and (got[skip + T:] == 0).all()
+    assert (k_pages[:at] == 0).all() and (vt_pages[:at] == 0).all()
