@@ -492,7 +492,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
     }
     const bool partial = sh.s.splits > 1;
     const int slot = sh.slot + sh.unit;
-    if (partial && slot >= part.n_slots) return;                // starts that are not ascending: more units than there is room for
+    if (partial && (unsigned)slot >= (unsigned)part.n_slots) return;                // starts that are not ascending: more units than there is room for
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
         if (f > 0) __syncthreads();
@@ -687,7 +687,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     const int n_st = min((cut + 1) * per, kt.n) - e0;                         // key tiles of this workgroup
     const bool partial = sh.s.splits > 1;
     const int slot = sh.slot + sh.unit;
-    if (partial && slot >= part.n_slots) return;
+    if (partial && (unsigned)slot >= (unsigned)part.n_slots) return;
 
     const int row = min(row0 + 32 * wave + l32, last_row);                    // rows past the last repeat it; they are not stored
     const bool valid = row0 + 32 * wave + l32 <= last_row;
@@ -1081,7 +1081,7 @@ __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& 
         const int kvh = sh.unit % a.Hkv, row = sh.unit / a.Hkv, splits = sh.s.splits;
         const int tile = row >> part.log_m, rt = row & (part.m - 1);
         const int slot0 = sh.slot + (sh.s.tiles - 1 - tile) * splits * a.Hkv + kvh;
-        if (slot0 + (splits - 1) * a.Hkv >= part.n_slots) continue;
+        if (slot0 < 0 || slot0 + (splits - 1) * a.Hkv >= part.n_slots) continue;
         auto at = [&](int s) { return (int64_t)(slot0 + s * a.Hkv) * part.m + rt; };
         float mx = -INFINITY, total = 0.f;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};

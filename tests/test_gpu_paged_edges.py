@@ -204,3 +204,40 @@ def test_append_of_many_tokens_far_past_32_bit_offsets(spa):
     for got, x in ((got_k, k), (got_v, v)):
         assert _same_bits(got[skip:skip + T], x) and (got[:skip] == 0).all() and (got[skip + T:] == 0).all()
     assert (k_pages[:at] == 0).all() and (vt_pages[:at] == 0).all()
+
+
+# --------------------------------------------------------------------------------- malformed lengths, next to other memory
+MALFORMED = [[0, 1, 2, 10 ** 9], [-5, 1, 2, 3], [0, 3, 1, 3], [2, 1, 0, 0], [0, 2 ** 31 - 1, -2 ** 31, 3], [0, 48, 0, 48], [48, 0, 48, 0]]
+
+
+@pytest.mark.parametrize("max_new", [0, 1, 48])
+@pytest.mark.parametrize("head_dim,q_heads", [(64, 4), (128, 20)])
+def test_malformed_lengths_of_calls_that_are_cut_change_nothing_around(spa, head_dim, q_heads, max_new):
+    """out, lse and workspace lie inside larger buffers: what is around them keeps its bits, for few and for many rows, in pieces and merged;
+    with sound starts the other requests are right whatever one request's length is."""
+    step = oracle.Step(2, [2600, 2400, 1900], [1, 40, 7], q_heads=q_heads, kv_heads=1, head_dim=head_dim, page=32)
+    T, Hq, D = step.q.shape
+    t = step.q.cuda(), step.k_pages.cuda(), step.vt_pages.cuda(), step.table.cuda()
+    n_pages, C, page = t[1].shape[0], t[3].shape[1], 32
+    p = spa.make_paged_params(batch=3, n_q_heads=Hq, n_kv_heads=1, head_dim=D, page_size=page, n_pages=n_pages, max_pages=C, n_tokens=T,
+                              max_new_tokens=max_new, table_stride=C, q=(Hq * D, D), out=(Hq * D, D), k_pages=(page * D, page * D),
+                              vt_pages=(page * D, page * D))
+    ws_bytes = spa.paged_workspace_bytes(p)
+    assert ws_bytes > 0
+    sizes = T * Hq * D * 2, T * Hq * 4, ws_bytes
+    margin = 1 << 16
+    want, want_lse, tol, lse_tol = step.want()
+    for starts, kv in [(s, step.kv_lens) for s in MALFORMED] + [(step.starts, [step.kv_lens[0], x, step.kv_lens[2]]) for x in (10 ** 9, -5, 0)]:
+        room = [torch.full((2 * margin + n,), 0xa5, dtype=torch.uint8, device="cuda") for n in sizes]
+        at = [x.data_ptr() + margin for x in room]
+        q_starts, kv_lens = _i32(starts), _i32(kv)
+        rc = spa.load_library().sparse_prefill_paged_attn(bytes(p), t[0].data_ptr(), t[1].data_ptr(), t[2].data_ptr(), t[3].data_ptr(), q_starts.data_ptr(),
+                                                          kv_lens.data_ptr(), None, at[0], at[1], at[2], ws_bytes, torch.cuda.current_stream().cuda_stream)
+        assert rc == 0
+        for x, n in zip(room, sizes):
+            assert (x[:margin] == 0xa5).all() and (x[margin + n:] == 0xa5).all(), (starts, kv)
+        if starts == step.starts:
+            out = room[0][margin:margin + sizes[0]].view(torch.bfloat16).view(T, Hq, D).cpu().double()
+            lse = room[1][margin:margin + sizes[1]].view(torch.float32).view(T, Hq).cpu().double()
+            rows = [0] + list(range(step.starts[2], T))
+            assert ((out - want).abs() <= tol)[rows].all() and ((lse - want_lse).abs() <= lse_tol)[rows].all()
