@@ -445,8 +445,9 @@ int sparse_prefill_paged_plan(const spa_paged_params *p, const int32_t *ctx_lens
 
 /* Keys and values of the new tokens into their pages: k, v [n_tokens, n_kv_heads, head_dim] (strides
  * k_stride, v_stride), token t to slots[t]; a slot outside the cache (-1 for padding) is passed over.  Every
- * other token of the cache keeps its bits.  A slot that occurs twice ends up with either token's values.  k and v
- * may not lie in the cache, nor K and V pages on each other.
+ * other token of the cache keeps its bits.  A slot is meant to occur once: where it occurs more often, each
+ * single value of its key and value is that of one of its tokens, but not of the same token throughout.
+ * k and v may not lie in the cache, nor K and V pages on each other.
  * Uses of p: n_kv_heads, head_dim, page_size, n_pages, n_tokens, strides. */
 int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const void *v, const int32_t *slots,
                                 void *k_pages, void *vt_pages, void *hip_stream);

@@ -133,7 +133,8 @@ def paged_plan(block_table, ctx_lens, new_lens, free_pages, free_range, n_tokens
 
 
 def paged_append(k, v, slots, k_pages, vt_pages):
-    """sparse_prefill_paged_append: k, v [n_tokens, n_kv_heads, head_dim] to the places slots (int32 [n_tokens]) of the cache."""
+    """sparse_prefill_paged_append: k, v [n_tokens, n_kv_heads, head_dim] to the places slots (int32 [n_tokens], each
+    once, or none: -1) of the cache."""
     n, h, page, d, k0, k1, v0, v1, dev = _cache(k_pages, vt_pages)
     T = slots.shape[0]
     if slots.dtype is not _I32 or slots.device != dev or slots.dim() != 1 or not slots.is_contiguous():

@@ -241,3 +241,21 @@ def test_malformed_lengths_of_calls_that_are_cut_change_nothing_around(spa, head
             lse = room[1][margin:margin + sizes[1]].view(torch.float32).view(T, Hq).cpu().double()
             rows = [0] + list(range(step.starts[2], T))
             assert ((out - want).abs() <= tol)[rows].all() and ((lse - want_lse).abs() <= lse_tol)[rows].all()
+
+
+@pytest.mark.parametrize("T", [60, 1500])
+def test_append_to_slots_that_occur_twice_leaves_values_of_their_tokens(spa, T):
+    """Each value one of the tokens' own, whichever; nothing else changes."""
+    N, H, D, page = 60, 2, 64, 32
+    half = T // 2
+    for again in (list(range(3, 3 + half)), list(range(10, 10 + half)), list(range(2 + half, 2, -1))):
+        slots = list(range(3, 3 + half)) + again
+        k, v = _bits(T, H, D, seed=1), _bits(T, H, D, seed=2)
+        k_pages, vt_pages = _bits(N, H, page, D, seed=3), _bits(N, H, D, page, seed=4)
+        first = oracle.append(k, v, torch.tensor(slots), k_pages, vt_pages)
+        last = oracle.append(k.flip(0), v.flip(0), torch.tensor(slots).flip(0), k_pages, vt_pages)
+        mine = k_pages.cuda(), vt_pages.cuda()
+        spa.paged_append(k.cuda(), v.cuda(), _i32(slots), *mine)
+        for got, a, b in zip(mine, first, last):
+            got, a, b = (x.cpu().view(torch.int16) for x in (got, a, b))
+            assert ((got == a) | (got == b)).all()
