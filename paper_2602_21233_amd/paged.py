@@ -139,7 +139,11 @@ def paged_append(k, v, slots, k_pages, vt_pages):
     T = slots.shape[0]
     if slots.dtype is not _I32 or slots.device != dev or slots.dim() != 1 or not slots.is_contiguous():
         raise _bad_ints("slots", T, dev)
-    p = _pack(1, h, h, d, page, n, 1, T, 0, 0.0, 0, 0, 0.0, 1, 0, 0, *_rows("k", k, dev, T, h, d), *_rows("v", v, dev, T, h, d), 0, 0, k0, k1, v0, v1)
+    rows = *_rows("k", k, dev, T, h, d), *_rows("v", v, dev, T, h, d)
+    try:
+        p = _pack(1, h, h, d, page, n, 1, T, 0, 0.0, 0, 0, 0.0, 1, 0, 0, *rows, 0, 0, k0, k1, v0, v1)
+    except (struct.error, OverflowError):
+        raise _unfit() from None
     _launch("sparse_prefill_paged_append", dev, p, k.data_ptr(), v.data_ptr(), slots.data_ptr(), k_pages.data_ptr(), vt_pages.data_ptr())
 
 

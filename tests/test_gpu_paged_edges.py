@@ -259,3 +259,11 @@ def test_append_to_slots_that_occur_twice_leaves_values_of_their_tokens(spa, T):
         for got, a, b in zip(mine, first, last):
             got, a, b = (x.cpu().view(torch.int16) for x in (got, a, b))
             assert ((got == a) | (got == b)).all()
+
+
+def test_append_to_more_pages_than_a_field_holds_is_refused(spa):
+    k_pages = torch.zeros((1, 1, 16, 64), dtype=torch.bfloat16, device="cuda").expand(2 ** 31, 1, 16, 64)
+    vt_pages = torch.zeros((1, 1, 64, 16), dtype=torch.bfloat16, device="cuda").expand(2 ** 31, 1, 64, 16)
+    x = torch.zeros((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(spa.SpaError):
+        spa.paged_append(x, x, _i32([0]), k_pages, vt_pages)
