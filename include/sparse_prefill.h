@@ -403,7 +403,8 @@ typedef struct spa_paged_params {
     int32_t n_tokens;       /* 1 .. 2^24 rows of q, k, v, out, slots; n_tokens * n_q_heads < 2^31 */
     int32_t max_new_tokens; /* sparse_prefill_paged_attn: the most new tokens a request of the call
                                has, as far as the host knows (0: not known).  It chooses among
-                               kernels; results do not depend on it being right                 */
+                               kernels, and with them the rounding of weights below; results
+                               do not depend on it otherwise                                    */
     float softmax_scale;    /* 0 selects 1/sqrt(head_dim)                                       */
     int32_t n_sink_tokens;  /* >= 0 } with window_tokens = w > 0 the query at position i sees the keys */
     int32_t window_tokens;  /* >= 0 } j <= i with i - j < w or j < n_sink_tokens (the A-shape of
@@ -457,12 +458,13 @@ int sparse_prefill_paged_append(const spa_paged_params *p, const void *k, const 
  *   x_j = softmax_scale * q . k_j,  capped by softcap,  minus slopes[h] * (i - j),   over the keys j it sees
  *   out = sum_j softmax(x)_j v_j
  * in fp32 with bf16 matrix products; out [n_tokens, n_q_heads, head_dim] bf16.  Softmax weights enter the second product rounded to 16
- * bits for requests of few rows (new tokens * query heads of a KV head: up to 16 at least), to bf16 for others.  slopes_or_null: n_q_heads fp32
+ * bits in the kernel for few rows (new tokens * query heads of a KV head: up to 16, in some calls 32), to bf16 in the one for many.  slopes_or_null: n_q_heads fp32
  * on the device (bias by distance).  lse_or_null: [n_tokens, n_q_heads] fp32, ln sum_j e^x_j.  A query that
  * sees no key (kv_lens[b] = 0, or a position below 0) gets zeros and -inf, one that only sees keys with logits of -inf NaN and -inf.  What lies behind a request's last key, and
  * what no query of the call sees, may be anything, NaN too; a key that a query does not see has no influence on it,
  * whatever its key and value are.  A NaN value that a query sees makes its output NaN in that dim, an infinite one infinite, or NaN where
- * infinities of both signs meet or its weight is too small for fp32; however the call is cut.
+ * infinities of both signs meet or its weight is too small for fp32; however the call is cut.  Finite values are meant to be below 2^87: weights
+ * up to 2^40 are held before the division.
  * There is no attention in place: out may not lie on q.
  * ws: spa_paged_workspace_bytes() bytes, 256-byte aligned; its contents need not survive between calls, calls
  * that overlap in time need one each. */

@@ -81,8 +81,9 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v) {
     v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, true));
     return v;
 }
-// The kernel for many rows, up to 64 requests: of four lengths of a piece the one with the least time, by a model.  512 workgroups run
-// at once and take about 1.6 us a key tile: the longest piece, or the rounds of average ones, whichever is more; then the merge, 5 us and
+// The kernel for many rows, up to 64 requests: of four lengths of a piece the one with the least time, by a model.  512 workgroups that run
+// at once and take about 1.6 us a key tile (fitted with head_dim 128 without a cap, used for all: with head_dim 64 and a key tile in one page
+// 768 run at once): the longest piece, or the rounds of average ones, whichever is more; then the merge, 5 us and
 // 0.03 for each piece.  The lengths: no cut; as many pieces as run at once (each of the `tiles` row tiles and KV heads may end in a
 // short one); twice or four times as long, for short calls; or two rounds of pieces.  With 2^9 pieces always, or 2^10: chunk of
 // 2048 tokens 3040 / 3105 us, mixed step 493 / 455 (now 396); 180 tokens over 22000, 48 row tiles, in 528 pieces: 130 us, in 480: 98;
@@ -229,11 +230,12 @@ __device__ __forceinline__ float sum_over_groups(float v) { v += __shfl_xor(v, 1
 // v_mfma_f32_16x16x32_bf16 (S^T = K Q^T, O^T += V^T P^T).  A lane holds keys 8 (lane / 16) .. + 7 of a chunk of one row:
 // K rows are assigned to the first product's rows such that the weights are the second one's operand as they are.  Bound
 // by HBM: nothing is shared between the wavefronts, so there is no LDS in the loop and no barrier.
-// 64 requests of up to 8192 keys: 205 us for 1.14 GB of keys and values, 5.6 TB/s (a plain sum of 2 GiB: 6.07).
+// 64 requests of up to 8192 keys: 205 to 207 us for 1.14 GB of keys and values, 5.5 TB/s (a plain sum of 2 GiB: 6.07).
 //
 // NV > 1: a workgroup makes the outputs of D / NV dims only, from all of K and its share of V.  A CU takes in about 12 bytes a
 // clock however many loads it has in flight (256 KB of a head: 22000 cycles of a call of 501 keys), so a call of few workgroups
-// is faster on NV times as many, although they read K NV times: 11.8 -> 9.2 us.
+// is faster on NV times as many, although they read K NV times: 11.8 -> 9.2 us.  The host tells few workgroups from the table's width: the same
+// call in a table of 2048 pages takes 15.8.
 
 // LDS of a workgroup: the wavefronts' outputs, references and denominators
 template <int D, int MF, int NW, int NV>
@@ -550,8 +552,8 @@ __global__ __launch_bounds__(64 * NW, MF > 1 ? 2 : D == 64 ? 5 : 3) void paged_f
 // four share through LDS: the pipeline step of the sparse prefill's attention kernel (attn.hip: direct loads into a double
 // buffer, logits two 32-key chunks ahead of the second product, one barrier a tile), with pages in place of blocks, masks
 // where a tile needs them instead of in the last block, and logits that may be capped or biased.  2048 tokens over 98304 of 32 / 8
-// heads: 2.97 to 3.2 ms by card, 1.03 to 1.12 PFLOP/s (a plain product of 8192^3: 1.33), matrix cores busy 55 % at 1.8 GHz; with
-// head_dim 64, where the exponentials weigh twice as much, 0.84, capped 0.88 and 0.56.
+// heads: 2.97 to 3.2 ms by card, 1.03 to 1.12 PFLOP/s (a plain product of 8192^3: 1.33), matrix cores busy 56 % at 1.8 GHz; with
+// head_dim 64, where the exponentials weigh twice as much, 0.78 to 0.84, capped 0.88 to 0.91 and 0.56.
 // The keys are taken from the last tile to the first: with a bias that falls with the distance a row then meets its largest
 // logits first and its reference hardly moves.
 constexpr int kManyRows = 128;
@@ -1138,7 +1140,9 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a, PagedPart
 }
 
 // Most key tiles of a row tile, by the table's width and the window.  Where they are few, the merge's 5 us are more than pieces save
-// (4 tokens behind 1498 keys, window 76: 13.8 -> 9.4 us; 39 behind 1183, window 3: 15.4 -> 11.1).
+// (4 tokens behind 1498 keys, window 76: 13.8 -> 9.4 us; 39 behind 1183, window 3: 15.4 -> 11.1).  Few is 8; with 4 a request of 500 keys takes 13.0
+// instead of 9.2 us, 180 tokens over 500 22.9 instead of 19.3; with 16 a request of 750 keys 11.4 instead of 13.1, but of 1500 14.1 instead of
+// 13.0, and 180 tokens over 1000 30.5 instead of 28.1.
 int most_key_tiles_of(const PagedDims& d, const PagedPart& part) { return most_key_tiles(d.T, d.C << d.log_p, part.span, d.sink, d.window); }
 // Most workgroups of a part that a call can need, whatever its lengths (2^log_most more than without cuts, and none cut into pieces
 // of less than min_tiles)
