@@ -473,6 +473,76 @@ int sparse_prefill_paged_attn(const spa_paged_params *p, const void *q, const vo
                               const float *slopes_or_null, void *out, float *lse_or_null, void *ws,
                               size_t ws_bytes, void *hip_stream);
 
+/* ---- Quantised cache ---------------------------------------------------------------------------
+ * A paged cache of half the size.  Pages hold e4m3 values (8 bits: 4 of exponent, 3 of mantissa; infinities do not exist, NaN does) in
+ * place of bf16 ones, and every token has for each KV head one exponent for its key and one for its value:
+ *   k_pages   [n_pages, n_kv_heads, page_size, head_dim] e4m3,  k_exp [n_pages, n_kv_heads, page_size] uint8
+ *   vt_pages  [n_pages, n_kv_heads, head_dim, page_size] e4m3,  v_exp likewise
+ * A place stands for value * 2^(exponent - 127).  In these calls kp_stride and vp_stride count values of one byte; they are multiples of
+ * 16, as are the strides of the exponents.  The struct is read on the host, its pointers are device pointers. */
+typedef struct spa_paged_exps {
+    void *k;                /* uint8, 16-byte aligned; exponents 1 .. 254 (others give unspecified results   */
+    void *v;                /* for queries that see them)                                                    */
+    int64_t k_stride[2];    /* elements: page, head; multiples of 16, both >= page_size                      */
+    int64_t v_stride[2];
+} spa_paged_exps;
+
+/* Keys and values of the new tokens (bf16) into quantised pages: sparse_prefill_paged_append with, for each token and KV head and for
+ * key and value apart, the exponent e that is the least with max |x_d| <= 448 * 2^e over the finite x_d (at least -126, and -126
+ * where all are 0); the page gets x_d 2^-e rounded to the nearest e4m3 value, ties to even, and the exponent's place e + 127.  A power of two
+ * makes both the quotient and the value that is read back exact, and e4m3 keeps its precision down to 2^-14 of the row's maximum.
+ * Infinities and NaN become NaN.  Values are meant to be below 2^119: larger ones may stand for more than bf16 holds.
+ * Uses of p: n_kv_heads, head_dim, page_size, n_pages, n_tokens, strides. */
+int sparse_prefill_paged_append_q8(const spa_paged_params *p, const void *k, const void *v, const int32_t *slots,
+                                   void *k_pages, void *vt_pages, const spa_paged_exps *exps, void *hip_stream);
+
+/* sparse_prefill_paged_attn over a quantised cache: the same sums over the values that pages and exponents stand for, which enter the
+ * matrix products exactly; same options, precision, workspace (spa_paged_workspace_bytes) and treatment of what is not finite or not seen.
+ * What lies behind a request's last key may be anything here, too, exponents among it. */
+int sparse_prefill_paged_attn_q8(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,
+                                 const spa_paged_exps *exps, const int32_t *block_table, const int32_t *q_starts,
+                                 const int32_t *kv_lens, const float *slopes_or_null, void *out, float *lse_or_null,
+                                 void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Cached tokens back out of their pages, as bf16 rows k, v [n_tokens, n_kv_heads, head_dim] (strides k_stride, v_stride, both >=
+ * head_dim: with strides of a [heads, tokens, dim] tensor they are the K and V that sparse_prefill_fused takes for a chunk behind a
+ * cached prefix).  starts [batch + 1]: request b has the rows starts[b] .. starts[b + 1] - 1, which are its last tokens, so that row i of n has
+ * position kv_lens[b] - n + i (n = kv_lens[b]: all of it).  Rows with a position below 0 get zeros; rows behind the last one are left as
+ * they were.  exps_or_null: NULL for a cache of bf16 pages, whose bits are copied; else values are as above, exact in bf16.
+ * Uses of p: batch, n_kv_heads, head_dim, page_size, n_pages, max_pages, n_tokens, table_stride, strides. */
+int sparse_prefill_paged_read(const spa_paged_params *p, const void *k_pages, const void *vt_pages,
+                              const spa_paged_exps *exps_or_null, const int32_t *block_table, const int32_t *starts,
+                              const int32_t *kv_lens, void *k, void *v, void *hip_stream);
+
+/* ---- Shared prompts ----------------------------------------------------------------------------
+ * Requests whose first tokens are the same keep them in the same pages.  shares [3, batch] int32 says which: groups are runs of consecutive
+ * requests;
+ *   shares[0][b]  first request of b's group
+ *   shares[1][b]  requests of the group (1: b shares nothing)
+ *   shares[2][b]  tokens that they have in common, in common pages (0 for a group of one)
+ * the same values for every request of a group.
+ *
+ * sparse_prefill_paged_shares finds the groups in the block tables.  c[b], b > 0: tokens of the leading columns that are equal in rows b - 1 and
+ * b, among those that both requests filled with cached tokens (kv_lens less new ones), c[0] = c[batch] = 0.  Request b joins the one before it if
+ * c[b] >= max(min_tokens, 1) and 2 c[b] >= max(c[b - 1], c[b + 1]): it does not when one of the two has more than twice as much in common with its other
+ * neighbour.  A group's shares[2] is its least c.  Other groups may be written by hand.  min_tokens < 0: SPA_ERR_BAD_PATTERN.
+ * Uses of p: batch, page_size, max_pages, n_tokens, table_stride. */
+int sparse_prefill_paged_shares(const spa_paged_params *p, const int32_t *block_table, const int32_t *q_starts,
+                                const int32_t *kv_lens, int32_t min_tokens, int32_t *shares, void *hip_stream);
+
+/* Bytes of device scratch that sparse_prefill_paged_attn_shared needs in `ws`.  Host only. */
+int spa_paged_shared_workspace_bytes(const spa_paged_params *p, size_t *bytes);
+
+/* sparse_prefill_paged_attn (exps_or_null NULL) or sparse_prefill_paged_attn_q8 for requests that share prompts: the same sums, but the queries of
+ * a group attend together to what they have in common, which is read once for all of them through the table row of the group's first request,
+ * and each request to the rest by itself; the parts are joined by their log-sum-exps.  shares: as above, read on the device; where the rows of
+ * a group do not have shares[2] tokens in common pages its results are unspecified. */
+int sparse_prefill_paged_attn_shared(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,
+                                     const spa_paged_exps *exps_or_null, const int32_t *block_table,
+                                     const int32_t *q_starts, const int32_t *kv_lens, const int32_t *shares,
+                                     const float *slopes_or_null, void *out, float *lse_or_null, void *ws,
+                                     size_t ws_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,7 +19,8 @@ EXPORTS = ("spa_strerror", "spa_row_capacity", "spa_workspace_bytes", "sparse_pr
            "sparse_prefill_fused_stem", "sparse_prefill_select_ex", "sparse_prefill_topk_from_scores_ex",
            "sparse_prefill_fused_ex", "sparse_prefill_check_lists", "sparse_prefill_select_static",
            "sparse_prefill_transpose_v", "sparse_prefill_attn_vt", "spa_paged_workspace_bytes", "sparse_prefill_paged_plan",
-           "sparse_prefill_paged_append", "sparse_prefill_paged_attn")
+           "sparse_prefill_paged_append", "sparse_prefill_paged_attn", "sparse_prefill_paged_append_q8", "sparse_prefill_paged_attn_q8",
+           "sparse_prefill_paged_read", "sparse_prefill_paged_shares", "spa_paged_shared_workspace_bytes", "sparse_prefill_paged_attn_shared")
 
 
 class SpaError(RuntimeError):
@@ -57,6 +58,10 @@ class SpaPagedParams(ctypes.Structure):
     _fields_ += [("softmax_scale", ctypes.c_float), ("n_sink_tokens", ctypes.c_int32), ("window_tokens", ctypes.c_int32),
                  ("softcap", ctypes.c_float), ("table_stride", ctypes.c_int64)]
     _fields_ += [(n + "_stride", ctypes.c_int64 * 2) for n in ("q", "k", "v", "o", "kp", "vp")]
+
+
+class SpaPagedExps(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2)]
 
 
 def library_path() -> str:
@@ -100,6 +105,12 @@ def load_library():
     lib.sparse_prefill_paged_plan.argtypes = [vp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.sparse_prefill_paged_append.argtypes = [vp, vp, vp, vp, vp, vp, vp]
     lib.sparse_prefill_paged_attn.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.sparse_prefill_paged_append_q8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sparse_prefill_paged_attn_q8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.sparse_prefill_paged_read.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sparse_prefill_paged_shares.argtypes = [vp, vp, vp, vp, ctypes.c_int32, vp, vp]
+    lib.spa_paged_shared_workspace_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
+    lib.sparse_prefill_paged_attn_shared.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     for name in EXPORTS[1:]:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib

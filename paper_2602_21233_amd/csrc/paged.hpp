@@ -16,6 +16,12 @@ struct PagedDims {
     int64_t q_t, q_h, o_t, o_h, kp_p, kp_h, vp_p, vp_h;
 };
 
+// Exponents of a quantised cache; no k: the pages hold bf16 values
+struct PagedExps {
+    uint8_t *k, *v;
+    int64_t k_p, k_h, v_p, v_h;
+};
+
 // One of the two attention kernels.  It serves the requests with row_lo < rows <= row_hi, rows = new tokens * query heads of a
 // KV head, m = 2^log_m rows a workgroup (0: no such kernel in the call), which span at most `span` tokens, and cuts the key axis
 // into pieces: of at least `min_tiles` key tiles, and so that at most 2^log_most of them come about beyond one for every row tile.
@@ -107,5 +113,17 @@ PagedParts paged_parts(const PagedDims& d, void* ws_or_null);
 hipError_t launch_paged_attn(const PagedDims& d, const PagedParts& parts, const void* q, const void* k_pages, const void* vt_pages,
                              const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens, const float* slopes_or_null,
                              void* out, float* lse_or_null, hipStream_t st);
+
+// The quantised cache, and shared prompts
+hipError_t launch_paged_append_q8(const PagedDims& d, const void* k, int64_t k_t, int64_t k_h, const void* v, int64_t v_t, int64_t v_h,
+                                  const int32_t* slots, void* k_pages, void* vt_pages, const PagedExps& exps, hipStream_t st);
+hipError_t launch_paged_read(const PagedDims& d, const void* k_pages, const void* vt_pages, const PagedExps& exps, const int32_t* block_table,
+                             const int32_t* starts, const int32_t* kv_lens, void* k, int64_t k_t, int64_t k_h, void* v, int64_t v_t, int64_t v_h,
+                             hipStream_t st);
+hipError_t launch_paged_shares(const PagedDims& d, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens, int min_tokens,
+                               int32_t* shares, hipStream_t st);
+hipError_t launch_paged_plainly(const PagedDims& d, const void* q, const void* k_pages, const void* vt_pages, const PagedExps& exps,
+                                const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens, const float* slopes_or_null, void* out,
+                                float* lse_or_null, hipStream_t st);
 
 }  // namespace spa

@@ -1,5 +1,6 @@
 """Binding of the paged-KV-cache calls of include/sparse_prefill.h: block tables and slot maps of a serving step, the new
-tokens' keys and values into their pages, attention over the pages.  Argument marshalling only; a step makes these calls for
+tokens' keys and values into their pages, attention over the pages; the same for quantised pages, cached tokens back out of either, requests
+that share prompts.  Argument marshalling only; a step makes these calls for
 every layer and is short, so they are written for few Python operations."""
 from __future__ import annotations
 
@@ -10,13 +11,15 @@ import struct
 import torch
 
 from . import binding
-from .binding import SpaError, SpaPagedParams, _check, _raw_stream, load_library
+from .binding import SpaError, SpaPagedExps, SpaPagedParams, _check, _raw_stream, load_library
 
 # 9 int32, a float, 2 int32, a float, table_stride and six stride pairs: see SpaPagedParams
 _PARAMS = struct.Struct("@9if2if13q")
 assert _PARAMS.size == ctypes.sizeof(SpaPagedParams)
 _pack = _PARAMS.pack
-_I32, _BF16 = torch.int32, torch.bfloat16
+_EXPS = struct.Struct("@2P4q")                   # two addresses and two stride pairs: see SpaPagedExps
+assert _EXPS.size == ctypes.sizeof(SpaPagedExps)
+_I32, _BF16, _E4M3 = torch.int32, torch.bfloat16, torch.float8_e4m3fn
 
 
 def _unfit():
@@ -75,14 +78,14 @@ def _rows(name, t, device, n, heads, dim):
     return (token if n > 1 else heads * head), head
 
 
-def _cache(k_pages, vt_pages):
+def _cache(k_pages, vt_pages, dtype=_BF16):
     """(n_pages, n_kv_heads, page_size, head_dim, K's page and head strides, V's, device)"""
     if k_pages.dim() != 4:
         raise TypeError("k_pages must be [n_pages, n_kv_heads, page_size, head_dim]")
     n, h, p, d = k_pages.shape
     device = k_pages.device
-    if k_pages.dtype is not _BF16 or vt_pages.dtype is not _BF16 or not k_pages.is_cuda or vt_pages.device != device:
-        raise TypeError("k_pages and vt_pages must be bf16 tensors on one GPU")
+    if k_pages.dtype is not dtype or vt_pages.dtype is not dtype or not k_pages.is_cuda or vt_pages.device != device:
+        raise TypeError(f"k_pages and vt_pages must be {'bf16' if dtype is _BF16 else 'float8_e4m3fn'} tensors on one GPU")
     k0, k1, k2, k3 = k_pages.stride()
     v0, v1, v2, v3 = vt_pages.stride()
     if vt_pages.shape != (n, h, d, p) or k3 != 1 or k2 != d or v3 != 1 or v2 != p:
@@ -93,6 +96,21 @@ def _cache(k_pages, vt_pages):
     if n == 1:
         k0, v0 = h * k1, h * v1
     return n, h, p, d, k0, k1, v0, v1, device
+
+
+def _exps(k_exp, v_exp, device, n, h, p):
+    """The packed SpaPagedExps of the exponents of a cache."""
+    at = []
+    for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
+        if t is None or t.dtype is not torch.uint8 or t.device != device or t.shape != (n, h, p):
+            raise TypeError(f"{name} must be a uint8 tensor [{n}, {h}, {p}] on {device}")
+        page, head, inner = t.stride()
+        if inner != 1:
+            raise TypeError(f"the last axis of {name} must be contiguous")
+        if h == 1:
+            head = p
+        at += [page if n > 1 else h * head, head]
+    return _EXPS.pack(k_exp.data_ptr(), v_exp.data_ptr(), *at)
 
 
 def _launch(name, device, *args):
@@ -152,14 +170,21 @@ def paged_attn(q, k_pages, vt_pages, block_table, q_starts, kv_lens, max_new_tok
     """sparse_prefill_paged_attn: q [n_tokens, n_q_heads, head_dim] -> out of the same shape (and lse [n_tokens, n_q_heads] fp32).
     max_new_tokens: the most new tokens of a request, where the host knows it (decode steps are up to an eighth faster with it); slopes: fp32 [n_q_heads], bias by distance.
     Rows of padding are left as they are in `out` (as allocated where none is given)."""
-    n, h, page, d, k0, k1, v0, v1, dev = _cache(k_pages, vt_pages)
+    return _attend("sparse_prefill_paged_attn", _workspace_bytes, _cache(k_pages, vt_pages), (), (), q, k_pages, vt_pages, block_table, q_starts,
+                   kv_lens, max_new_tokens, softmax_scale, n_sink_tokens, window_tokens, softcap, slopes, return_lse, out, workspace)
+
+
+def _attend(name, workspace_bytes, cache, after_pages, after_lens, q, k_pages, vt_pages, block_table, q_starts, kv_lens, max_new_tokens, softmax_scale,
+            n_sink_tokens, window_tokens, softcap, slopes, return_lse, out, workspace):
+    """The attention call `name`; after_pages, after_lens: its own arguments behind the pages and behind the lengths."""
+    n, h, page, d, k0, k1, v0, v1, dev = cache
     if q.dim() != 3 or kv_lens.dim() != 1:
         raise TypeError("q must be [n_tokens, n_q_heads, head_dim] and kv_lens [batch]")
     B = kv_lens.shape[0]
     T, Hq, _ = q.shape
-    for name, t, many in (("q_starts", q_starts, B + 1), ("kv_lens", kv_lens, B)):
+    for what, t, many in (("q_starts", q_starts, B + 1), ("kv_lens", kv_lens, B)):
         if t.dtype is not _I32 or t.device != dev or t.shape != (many,) or not t.is_contiguous():
-            raise _bad_ints(name, many, dev)
+            raise _bad_ints(what, many, dev)
     q_token, q_head = _rows("q", q, dev, T, Hq, d)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
@@ -176,14 +201,116 @@ def paged_attn(q, k_pages, vt_pages, block_table, q_starts, kv_lens, max_new_tok
         raise _unfit() from None
     lse = torch.empty((T, Hq), dtype=torch.float32, device=dev) if return_lse else None
     if workspace is None:
-        ws_bytes = _workspace_bytes(p)
+        ws_bytes = workspace_bytes(p)
         if ws_bytes:
             workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
     elif workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
         raise TypeError(f"workspace must be a contiguous uint8 tensor on {dev}")
     else:
         ws_bytes = workspace.numel()
-    _launch("sparse_prefill_paged_attn", dev, p, q.data_ptr(), k_pages.data_ptr(), vt_pages.data_ptr(), table, q_starts.data_ptr(),
-            kv_lens.data_ptr(), None if slopes is None else slopes.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
+    _launch(name, dev, p, q.data_ptr(), k_pages.data_ptr(), vt_pages.data_ptr(), *after_pages, table, q_starts.data_ptr(), kv_lens.data_ptr(),
+            *after_lens, None if slopes is None else slopes.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
             None if workspace is None else workspace.data_ptr(), ws_bytes)
     return (out, lse) if return_lse else out
+
+
+def paged_append_q8(k, v, slots, k_pages, vt_pages, k_exp, v_exp):
+    """sparse_prefill_paged_append_q8: bf16 k, v [n_tokens, n_kv_heads, head_dim] to the places slots of a quantised cache: float8_e4m3fn pages
+    and uint8 exponents k_exp, v_exp [n_pages, n_kv_heads, page_size]; a place stands for value * 2^(exponent - 127)."""
+    n, h, page, d, k0, k1, v0, v1, dev = _cache(k_pages, vt_pages, _E4M3)
+    T = slots.shape[0]
+    if slots.dtype is not _I32 or slots.device != dev or slots.dim() != 1 or not slots.is_contiguous():
+        raise _bad_ints("slots", T, dev)
+    rows = *_rows("k", k, dev, T, h, d), *_rows("v", v, dev, T, h, d)
+    exps = _exps(k_exp, v_exp, dev, n, h, page)
+    try:
+        p = _pack(1, h, h, d, page, n, 1, T, 0, 0.0, 0, 0, 0.0, 1, 0, 0, *rows, 0, 0, k0, k1, v0, v1)
+    except (struct.error, OverflowError):
+        raise _unfit() from None
+    _launch("sparse_prefill_paged_append_q8", dev, p, k.data_ptr(), v.data_ptr(), slots.data_ptr(), k_pages.data_ptr(), vt_pages.data_ptr(), exps)
+
+
+def paged_attn_q8(q, k_pages, vt_pages, k_exp, v_exp, block_table, q_starts, kv_lens, max_new_tokens=0, softmax_scale=None, n_sink_tokens=0,
+                  window_tokens=0, softcap=0.0, slopes=None, return_lse=False, out=None, workspace=None):
+    """sparse_prefill_paged_attn_q8: paged_attn over the quantised cache of paged_append_q8."""
+    cache = _cache(k_pages, vt_pages, _E4M3)
+    n, h, page, _, _, _, _, _, dev = cache
+    return _attend("sparse_prefill_paged_attn_q8", _workspace_bytes, cache, (_exps(k_exp, v_exp, dev, n, h, page),), (), q, k_pages, vt_pages,
+                   block_table, q_starts, kv_lens, max_new_tokens, softmax_scale, n_sink_tokens, window_tokens, softcap, slopes, return_lse, out, workspace)
+
+
+def paged_read(k_pages, vt_pages, block_table, starts, kv_lens, n_tokens, k_exp=None, v_exp=None, k=None, v=None):
+    """sparse_prefill_paged_read: the last starts[b + 1] - starts[b] cached tokens of every request as bf16 rows (k, v), both [n_tokens, n_kv_heads,
+    head_dim], out of bf16 pages, or quantised ones with k_exp and v_exp.  Rows behind the last one are left as they are (as allocated where no k, v
+    are given).  k[0].transpose(0, 1) of a sparse prefill's [1, heads, tokens, dim] tensors is a place for them."""
+    q8 = k_exp is not None or v_exp is not None
+    n, h, page, d, k0, k1, v0, v1, dev = _cache(k_pages, vt_pages, _E4M3 if q8 else _BF16)
+    if kv_lens.dim() != 1:
+        raise TypeError("kv_lens must be [batch]")
+    B = kv_lens.shape[0]
+    for name, t, many in (("starts", starts, B + 1), ("kv_lens", kv_lens, B)):
+        if t.dtype is not _I32 or t.device != dev or t.shape != (many,) or not t.is_contiguous():
+            raise _bad_ints(name, many, dev)
+    if n_tokens < 0:
+        raise _unfit()
+    new = lambda: torch.empty((n_tokens, h, d), dtype=_BF16, device=dev)  # noqa: E731
+    k, v = new() if k is None else k, new() if v is None else v
+    rows = *_rows("k", k, dev, n_tokens, h, d), *_rows("v", v, dev, n_tokens, h, d)
+    exps = _exps(k_exp, v_exp, dev, n, h, page) if q8 else None
+    table, columns, stride = _table(block_table, dev, B)
+    try:
+        p = _pack(B, h, h, d, page, n, columns, n_tokens, 0, 0.0, 0, 0, 0.0, stride, 0, 0, *rows, 0, 0, k0, k1, v0, v1)
+    except (struct.error, OverflowError):
+        raise _unfit() from None
+    _launch("sparse_prefill_paged_read", dev, p, k_pages.data_ptr(), vt_pages.data_ptr(), exps, table, starts.data_ptr(), kv_lens.data_ptr(),
+            k.data_ptr(), v.data_ptr())
+    return k, v
+
+
+def paged_shares(block_table, q_starts, kv_lens, page_size, min_tokens=512):
+    """sparse_prefill_paged_shares: int32 [3, batch], for every request the first one of its group, how many the group has, and the tokens that
+    they have in common (at least min_tokens)."""
+    dev = kv_lens.device
+    if not kv_lens.is_cuda or kv_lens.dim() != 1:
+        raise TypeError("kv_lens must be [batch] on the GPU")
+    B = kv_lens.shape[0]
+    for name, t, many in (("q_starts", q_starts, B + 1), ("kv_lens", kv_lens, B)):
+        if t.dtype is not _I32 or t.device != dev or t.shape != (many,) or not t.is_contiguous():
+            raise _bad_ints(name, many, dev)
+    table, columns, stride = _table(block_table, dev, B)
+    try:
+        p = _pack(B, 1, 1, 64, page_size, 1, columns, 1 << 24, 0, 0.0, 0, 0, 0.0, stride, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+        least = ctypes.c_int32(min_tokens) if -2 ** 31 <= min_tokens < 2 ** 31 else None
+    except (struct.error, OverflowError):
+        raise _unfit() from None
+    if least is None:
+        raise _unfit()
+    shares = torch.empty((3, B), dtype=_I32, device=dev)
+    _launch("sparse_prefill_paged_shares", dev, p, table, q_starts.data_ptr(), kv_lens.data_ptr(), least, shares.data_ptr())
+    return shares
+
+
+def paged_shared_workspace_bytes(p: SpaPagedParams) -> int:
+    """sparse_prefill_paged_attn_shared's scratch for these parameters."""
+    return _shared_workspace_bytes(bytes(p))
+
+
+@functools.lru_cache(maxsize=256)
+def _shared_workspace_bytes(packed: bytes) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().spa_paged_shared_workspace_bytes(packed, ctypes.byref(n)))
+    return n.value
+
+
+def paged_attn_shared(q, k_pages, vt_pages, block_table, q_starts, kv_lens, shares, k_exp=None, v_exp=None, max_new_tokens=0, softmax_scale=None,
+                      n_sink_tokens=0, window_tokens=0, softcap=0.0, slopes=None, return_lse=False, out=None, workspace=None):
+    """sparse_prefill_paged_attn_shared: paged_attn, or with k_exp and v_exp paged_attn_q8, for requests that share prompts as shares
+    (int32 [3, batch], from paged_shares) says; what a group has in common is read once."""
+    q8 = k_exp is not None or v_exp is not None
+    cache = _cache(k_pages, vt_pages, _E4M3 if q8 else _BF16)
+    n, h, page, _, _, _, _, _, dev = cache
+    if kv_lens.dim() != 1 or shares.dtype is not _I32 or shares.device != dev or shares.shape != (3, kv_lens.shape[0]) or not shares.is_contiguous():
+        raise TypeError(f"shares must be a contiguous int32 tensor [3, batch] on {dev}")
+    return _attend("sparse_prefill_paged_attn_shared", _shared_workspace_bytes, cache, (_exps(k_exp, v_exp, dev, n, h, page) if q8 else None,),
+                   (shares.data_ptr(),), q, k_pages, vt_pages, block_table, q_starts, kv_lens, max_new_tokens, softmax_scale, n_sink_tokens,
+                   window_tokens, softcap, slopes, return_lse, out, workspace)
