@@ -122,6 +122,9 @@ hipError_t launch_paged_read(const PagedDims& d, const void* k_pages, const void
                              hipStream_t st);
 hipError_t launch_paged_shares(const PagedDims& d, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens, int min_tokens,
                                int32_t* shares, hipStream_t st);
+hipError_t launch_paged_attn_q8(const PagedDims& d, const PagedParts& parts, const void* q, const void* k_pages, const void* vt_pages,
+                                const PagedExps& exps, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens,
+                                const float* slopes_or_null, void* out, float* lse_or_null, hipStream_t st);
 hipError_t launch_paged_plainly(const PagedDims& d, const void* q, const void* k_pages, const void* vt_pages, const PagedExps& exps,
                                 const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens, const float* slopes_or_null, void* out,
                                 float* lse_or_null, hipStream_t st);

@@ -98,7 +98,8 @@ int attend(const spa_paged_params* p, const void* q, const void* k_pages, const 
     if ((rc = check_table(p))) return rc;
     if ((rc = check_strided(q, p->q_stride, 0)) || (rc = check_strided(out, p->o_stride, p->head_dim)) || (rc = check_pages(p, k_pages, vt_pages, exps))) return rc;
     const PagedDims d = paged_dims(p);
-    const size_t need = shared ? 0 : paged_parts(d, ws).ws_bytes;
+    const PagedParts parts = paged_parts(d, ws);
+    const size_t need = shared ? 0 : parts.ws_bytes;
     if (need > 0 && !ws) return SPA_ERR_NULLPTR;
     if (((uintptr_t)ws) & 255u) return SPA_ERR_BAD_STRIDE;
     if (ws_bytes < need) return SPA_ERR_WORKSPACE_TOO_SMALL;
@@ -110,6 +111,9 @@ int attend(const spa_paged_params* p, const void* q, const void* k_pages, const 
     const Rows written[] = {token_rows(p, out, p->o_stride, p->n_q_heads), words_of(lse_or_null, (int64_t)p->n_tokens * p->n_q_heads),
                             row_of(ws, (int64_t)need)};
     if (clash(written, read) || k_pages == vt_pages || (exps && exps->k == exps->v)) return SPA_ERR_OVERLAP;
+    if (!shared)
+        return launch_code(launch_paged_attn_q8(d, parts, q, k_pages, vt_pages, paged_exps(exps), block_table, q_starts, kv_lens, slopes_or_null, out,
+                                                lse_or_null, (hipStream_t)hip_stream));
     return launch_code(launch_paged_plainly(d, q, k_pages, vt_pages, paged_exps(exps), block_table, q_starts, kv_lens, slopes_or_null, out, lse_or_null,
                                             (hipStream_t)hip_stream));
 }
