@@ -493,13 +493,13 @@ typedef struct spa_paged_exps {
  * makes both the quotient and the value that is read back exact, and e4m3 keeps its precision down to 2^-14 of the row's maximum.
  * Infinities and NaN become NaN.  Values are meant to be below 2^119: larger ones may stand for more than bf16 holds.
  * Uses of p: n_kv_heads, head_dim, page_size, n_pages, n_tokens, strides. */
-int sparse_prefill_paged_append_q8(const spa_paged_params *p, const void *k, const void *v, const int32_t *slots,
+int sparse_prefill_paged_append_quantised(const spa_paged_params *p, const void *k, const void *v, const int32_t *slots,
                                    void *k_pages, void *vt_pages, const spa_paged_exps *exps, void *hip_stream);
 
 /* sparse_prefill_paged_attn over a quantised cache: the same sums over the values that pages and exponents stand for, which enter the
  * matrix products exactly; same options, precision, workspace (spa_paged_workspace_bytes) and treatment of what is not finite or not seen.
  * What lies behind a request's last key may be anything here, too, exponents among it. */
-int sparse_prefill_paged_attn_q8(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,
+int sparse_prefill_paged_attn_quantised(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,
                                  const spa_paged_exps *exps, const int32_t *block_table, const int32_t *q_starts,
                                  const int32_t *kv_lens, const float *slopes_or_null, void *out, float *lse_or_null,
                                  void *ws, size_t ws_bytes, void *hip_stream);
@@ -533,7 +533,7 @@ int sparse_prefill_paged_shares(const spa_paged_params *p, const int32_t *block_
 /* Bytes of device scratch that sparse_prefill_paged_attn_shared needs in `ws`.  Host only. */
 int spa_paged_shared_workspace_bytes(const spa_paged_params *p, size_t *bytes);
 
-/* sparse_prefill_paged_attn (exps_or_null NULL) or sparse_prefill_paged_attn_q8 for requests that share prompts: the same sums, but the queries of
+/* sparse_prefill_paged_attn (exps_or_null NULL) or sparse_prefill_paged_attn_quantised for requests that share prompts: the same sums, but the queries of
  * a group attend together to what they have in common, which is read once for all of them through the table row of the group's first request,
  * and each request to the rest by itself; the parts are joined by their log-sum-exps.  shares: as above, read on the device; where the rows of
  * a group do not have shares[2] tokens in common pages its results are unspecified. */

@@ -19,7 +19,7 @@ EXPORTS = ("spa_strerror", "spa_row_capacity", "spa_workspace_bytes", "sparse_pr
            "sparse_prefill_fused_stem", "sparse_prefill_select_ex", "sparse_prefill_topk_from_scores_ex",
            "sparse_prefill_fused_ex", "sparse_prefill_check_lists", "sparse_prefill_select_static",
            "sparse_prefill_transpose_v", "sparse_prefill_attn_vt", "spa_paged_workspace_bytes", "sparse_prefill_paged_plan",
-           "sparse_prefill_paged_append", "sparse_prefill_paged_attn", "sparse_prefill_paged_append_q8", "sparse_prefill_paged_attn_q8",
+           "sparse_prefill_paged_append", "sparse_prefill_paged_attn", "sparse_prefill_paged_append_quantised", "sparse_prefill_paged_attn_quantised",
            "sparse_prefill_paged_read", "sparse_prefill_paged_shares", "spa_paged_shared_workspace_bytes", "sparse_prefill_paged_attn_shared")
 
 
@@ -105,8 +105,8 @@ def load_library():
     lib.sparse_prefill_paged_plan.argtypes = [vp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.sparse_prefill_paged_append.argtypes = [vp, vp, vp, vp, vp, vp, vp]
     lib.sparse_prefill_paged_attn.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
-    lib.sparse_prefill_paged_append_q8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
-    lib.sparse_prefill_paged_attn_q8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.sparse_prefill_paged_append_quantised.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sparse_prefill_paged_attn_quantised.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.sparse_prefill_paged_read.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.sparse_prefill_paged_shares.argtypes = [vp, vp, vp, vp, ctypes.c_int32, vp, vp]
     lib.spa_paged_shared_workspace_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]

@@ -188,7 +188,7 @@ int sparse_prefill_paged_attn(const spa_paged_params* p, const void* q, const vo
                                          (hipStream_t)hip_stream));
 }
 
-int sparse_prefill_paged_append_q8(const spa_paged_params* p, const void* k, const void* v, const int32_t* slots, void* k_pages,
+int sparse_prefill_paged_append_quantised(const spa_paged_params* p, const void* k, const void* v, const int32_t* slots, void* k_pages,
                                    void* vt_pages, const spa_paged_exps* exps, void* hip_stream) {
     int rc = check_paged(p);
     if (rc) return rc;
@@ -201,7 +201,7 @@ int sparse_prefill_paged_append_q8(const spa_paged_params* p, const void* k, con
                                               vt_pages, paged_exps(exps), (hipStream_t)hip_stream));
 }
 
-int sparse_prefill_paged_attn_q8(const spa_paged_params* p, const void* q, const void* k_pages, const void* vt_pages, const spa_paged_exps* exps,
+int sparse_prefill_paged_attn_quantised(const spa_paged_params* p, const void* q, const void* k_pages, const void* vt_pages, const spa_paged_exps* exps,
                                  const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens, const float* slopes_or_null,
                                  void* out, float* lse_or_null, void* ws, size_t ws_bytes, void* hip_stream) {
     const int rc = check_paged(p);

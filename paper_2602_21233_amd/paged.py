@@ -215,7 +215,7 @@ def _attend(name, workspace_bytes, cache, after_pages, after_lens, q, k_pages, v
 
 
 def paged_append_q8(k, v, slots, k_pages, vt_pages, k_exp, v_exp):
-    """sparse_prefill_paged_append_q8: bf16 k, v [n_tokens, n_kv_heads, head_dim] to the places slots of a quantised cache: float8_e4m3fn pages
+    """sparse_prefill_paged_append_quantised: bf16 k, v [n_tokens, n_kv_heads, head_dim] to the places slots of a quantised cache: float8_e4m3fn pages
     and uint8 exponents k_exp, v_exp [n_pages, n_kv_heads, page_size]; a place stands for value * 2^(exponent - 127)."""
     n, h, page, d, k0, k1, v0, v1, dev = _cache(k_pages, vt_pages, _E4M3)
     T = slots.shape[0]
@@ -227,15 +227,15 @@ def paged_append_q8(k, v, slots, k_pages, vt_pages, k_exp, v_exp):
         p = _pack(1, h, h, d, page, n, 1, T, 0, 0.0, 0, 0, 0.0, 1, 0, 0, *rows, 0, 0, k0, k1, v0, v1)
     except (struct.error, OverflowError):
         raise _unfit() from None
-    _launch("sparse_prefill_paged_append_q8", dev, p, k.data_ptr(), v.data_ptr(), slots.data_ptr(), k_pages.data_ptr(), vt_pages.data_ptr(), exps)
+    _launch("sparse_prefill_paged_append_quantised", dev, p, k.data_ptr(), v.data_ptr(), slots.data_ptr(), k_pages.data_ptr(), vt_pages.data_ptr(), exps)
 
 
 def paged_attn_q8(q, k_pages, vt_pages, k_exp, v_exp, block_table, q_starts, kv_lens, max_new_tokens=0, softmax_scale=None, n_sink_tokens=0,
                   window_tokens=0, softcap=0.0, slopes=None, return_lse=False, out=None, workspace=None):
-    """sparse_prefill_paged_attn_q8: paged_attn over the quantised cache of paged_append_q8."""
+    """sparse_prefill_paged_attn_quantised: paged_attn over the quantised cache of paged_append_q8."""
     cache = _cache(k_pages, vt_pages, _E4M3)
     n, h, page, _, _, _, _, _, dev = cache
-    return _attend("sparse_prefill_paged_attn_q8", _workspace_bytes, cache, (_exps(k_exp, v_exp, dev, n, h, page),), (), q, k_pages, vt_pages,
+    return _attend("sparse_prefill_paged_attn_quantised", _workspace_bytes, cache, (_exps(k_exp, v_exp, dev, n, h, page),), (), q, k_pages, vt_pages,
                    block_table, q_starts, kv_lens, max_new_tokens, softmax_scale, n_sink_tokens, window_tokens, softcap, slopes, return_lse, out, workspace)
 
 
