@@ -33,6 +33,7 @@ struct PagedPart {
     int n_slots;                      // partial results that the workspace has room for; 0: nothing is cut
     float *o, *lse;                   // partial results: [n_slots][m][D], [n_slots][m]; lse in base 2
     int32_t* piece;                   // many rows: key tiles of a piece, as the attention kernel leaves them for the merge
+    int32_t* unit_end;                // shared prompts: workgroups up to and with each of the call's 2 B shares
 };
 
 // A request's share of a part: row tiles, key tiles (of its longest row tile), pieces of the key axis
@@ -69,6 +70,21 @@ __host__ __device__ __forceinline__ int most_key_tiles(int q_len, int kv_len, in
     return some < all ? (int)some : all;
 }
 
+// The key tiles of a row tile among first .. end - 1: those of key_tiles that lie there, in the same order.
+struct KeyTilesWithin {
+    int first, sinks, from, n;
+    __host__ __device__ __forceinline__ int at(int e) const { return e < sinks ? e + first : e - sinks + from; }
+};
+__host__ __device__ __forceinline__ KeyTilesWithin key_tiles_within(int pos_lo, int pos_hi, int sink, int window, int first, int end) {
+    const KeyTiles all = key_tiles(pos_lo, pos_hi, sink, window);
+    const int last = pos_hi < 0 ? 0 : pos_hi / kPagedTile + 1, stop = end < last ? end : last;
+    KeyTilesWithin t{first, 0, all.from > first ? all.from : first, 0};
+    const int sinks = (all.sinks < stop ? all.sinks : stop) - first;
+    t.sinks = sinks > 0 ? sinks : 0;
+    t.n = t.sinks + (stop > t.from ? stop - t.from : 0);
+    return t;
+}
+
 constexpr int kWholeAxis = 1 << 24;   // key tiles: more than any key axis has
 __host__ __device__ __forceinline__ int piece_within(int64_t tiles, const PagedPart& part) {
     return tiles < part.min_tiles ? part.min_tiles : (tiles > kWholeAxis ? kWholeAxis : (int)tiles);
@@ -92,6 +108,27 @@ __host__ __device__ __forceinline__ PagedShare paged_share(const PagedPart& part
     if (rows > part.row_lo && rows <= part.row_hi) {
         s.tiles = (rows + part.m - 1) >> part.log_m;
         s.keys = most_key_tiles(q_len, kv_len, part.span, sink, window);
+        s.splits = s.keys <= piece ? 1 : (int)(((uint32_t)s.keys + (uint32_t)piece - 1u) / (uint32_t)piece);
+    }
+    return s;
+}
+
+// Shared prompts: share e < B is what group e (the one that starts at request e) has in common, share B + b the rest of request b.
+struct SharedRange {
+    int first, len;                   // rows of q: tokens of the group, or of the request
+    int tile, end;                    // key tiles tile .. end - 1
+    int b;                            // the request whose row of the table names the pages
+};
+// keys: cached tokens of the request (of no group: all that the group has in common); longest axis of any of its row tiles
+__host__ __device__ __forceinline__ PagedShare shared_share(const PagedPart& part, int G, const SharedRange& r, bool common, int kv_len, int sink, int window, int piece) {
+    PagedShare s{0, 0, 0};
+    const int64_t rows = (int64_t)r.len * G;
+    if (rows > part.row_lo && rows <= part.row_hi) {
+        const int all = (common ? r.end : (kv_len + kPagedTile - 1) / kPagedTile) - r.tile;
+        s.tiles = (int)((rows + part.m - 1) >> part.log_m);
+        s.keys = common ? all : most_key_tiles(r.len, kv_len, part.span, sink, window);
+        if (s.keys > all) s.keys = all;
+        if (s.keys < 0) s.keys = 0;
         s.splits = s.keys <= piece ? 1 : (int)(((uint32_t)s.keys + (uint32_t)piece - 1u) / (uint32_t)piece);
     }
     return s;
@@ -125,8 +162,13 @@ hipError_t launch_paged_shares(const PagedDims& d, const int32_t* block_table, c
 hipError_t launch_paged_attn_q8(const PagedDims& d, const PagedParts& parts, const void* q, const void* k_pages, const void* vt_pages,
                                 const PagedExps& exps, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens,
                                 const float* slopes_or_null, void* out, float* lse_or_null, hipStream_t st);
-hipError_t launch_paged_plainly(const PagedDims& d, const void* q, const void* k_pages, const void* vt_pages, const PagedExps& exps,
-                                const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens, const float* slopes_or_null, void* out,
-                                float* lse_or_null, hipStream_t st);
+// The parts of a call with shared prompts, and the arrays that its first kernel leaves for the others.
+PagedParts paged_shared_parts(const PagedDims& d, void* ws_or_null);
+hipError_t launch_paged_shared_q8(const PagedDims& d, const PagedParts& parts, const void* q, const void* k_pages, const void* vt_pages,
+                                  const PagedExps& exps, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens,
+                                  const int32_t* shares, const float* slopes_or_null, void* out, float* lse_or_null, hipStream_t st);
+hipError_t launch_paged_attn_shared(const PagedDims& d, const PagedParts& parts, const void* q, const void* k_pages, const void* vt_pages,
+                                    const PagedExps& exps, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens,
+                                    const int32_t* shares, const float* slopes_or_null, void* out, float* lse_or_null, hipStream_t st);
 
 }  // namespace spa

@@ -98,24 +98,23 @@ int attend(const spa_paged_params* p, const void* q, const void* k_pages, const 
     if ((rc = check_table(p))) return rc;
     if ((rc = check_strided(q, p->q_stride, 0)) || (rc = check_strided(out, p->o_stride, p->head_dim)) || (rc = check_pages(p, k_pages, vt_pages, exps))) return rc;
     const PagedDims d = paged_dims(p);
-    const PagedParts parts = paged_parts(d, ws);
-    const size_t need = shared ? 0 : parts.ws_bytes;
-    if (need > 0 && !ws) return SPA_ERR_NULLPTR;
+    const PagedParts parts = shared ? paged_shared_parts(d, ws) : paged_parts(d, ws);
+    if (parts.ws_bytes > 0 && !ws) return SPA_ERR_NULLPTR;
     if (((uintptr_t)ws) & 255u) return SPA_ERR_BAD_STRIDE;
-    if (ws_bytes < need) return SPA_ERR_WORKSPACE_TOO_SMALL;
+    if (ws_bytes < parts.ws_bytes) return SPA_ERR_WORKSPACE_TOO_SMALL;
     const int bytes = exps ? 1 : 2;
     // several workgroups read a query whose output one of them writes
     const Rows read[] = {token_rows(p, q, p->q_stride, p->n_q_heads), page_rows(p, k_pages, p->kp_stride, bytes), page_rows(p, vt_pages, p->vp_stride, bytes),
                          k_exp_rows(p, exps), v_exp_rows(p, exps), table_rows(p, block_table), words_of(q_starts, p->batch + 1), words_of(kv_lens, p->batch),
                          words_of(shares, 3ll * p->batch), words_of(slopes_or_null, p->n_q_heads)};
     const Rows written[] = {token_rows(p, out, p->o_stride, p->n_q_heads), words_of(lse_or_null, (int64_t)p->n_tokens * p->n_q_heads),
-                            row_of(ws, (int64_t)need)};
+                            row_of(ws, (int64_t)parts.ws_bytes)};
     if (clash(written, read) || k_pages == vt_pages || (exps && exps->k == exps->v)) return SPA_ERR_OVERLAP;
-    if (!shared)
-        return launch_code(launch_paged_attn_q8(d, parts, q, k_pages, vt_pages, paged_exps(exps), block_table, q_starts, kv_lens, slopes_or_null, out,
-                                                lse_or_null, (hipStream_t)hip_stream));
-    return launch_code(launch_paged_plainly(d, q, k_pages, vt_pages, paged_exps(exps), block_table, q_starts, kv_lens, slopes_or_null, out, lse_or_null,
-                                            (hipStream_t)hip_stream));
+    if (shared)
+        return launch_code(launch_paged_attn_shared(d, parts, q, k_pages, vt_pages, paged_exps(exps), block_table, q_starts, kv_lens, shares, slopes_or_null,
+                                                    out, lse_or_null, (hipStream_t)hip_stream));
+    return launch_code(launch_paged_attn_q8(d, parts, q, k_pages, vt_pages, paged_exps(exps), block_table, q_starts, kv_lens, slopes_or_null, out,
+                                            lse_or_null, (hipStream_t)hip_stream));
 }
 
 }  // namespace
@@ -243,7 +242,7 @@ int spa_paged_shared_workspace_bytes(const spa_paged_params* p, size_t* bytes) {
     const int rc = check_paged(p);
     if (rc) return rc;
     if (!bytes) return SPA_ERR_NULLPTR;
-    *bytes = 0;
+    *bytes = paged_shared_parts(paged_dims(p), nullptr).ws_bytes;
     return SPA_OK;
 }
 

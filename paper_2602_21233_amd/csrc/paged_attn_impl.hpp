@@ -39,6 +39,7 @@ struct PagedArgs {
     float scale, cap;                                 // cap 0: none
     int64_t table_stride, q_t, q_h, o_t, o_h, kp_p, kp_h, vp_p, vp_h;
     PagedExps exps;                                   // of a quantised cache
+    const int32_t* shares;                            // shared prompts: [3][B]
 };
 // a page value: bf16, or e4m3 (Q8)
 template <bool Q8>
@@ -180,6 +181,94 @@ __device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedPart& p
     }
     return found;
 }
+// ---------------------------------------------------------------------------------------------------------------
+// Shared prompts.  The rows of a group are the new tokens of its requests, which follow each other; they attend to the key tiles that the group has
+// in common, and each request's to its other ones.  A kernel of one workgroup (paged_attn_shared.hip) has cut the call: part.unit_end.  Every part
+// of a query that has more than one leaves a partial result, in the place of its workgroup.
+
+// whole key tiles in pages that the group of request b has in common, 0 where it has none; leader: its first request, n: how many there are
+struct Group {
+    int leader, n, tiles;
+};
+__device__ __forceinline__ Group group_of(const PagedArgs& a, int b) {
+    Group g;
+    g.leader = clamp_int(a.shares[b], 0, b);
+    g.n = clamp_int(a.shares[a.B + b], 0, a.B - g.leader);
+    const int tokens = clamp_int(a.shares[2 * (int64_t)a.B + b], 0, a.C << a.log_p);
+    g.tiles = g.n > 1 && b < g.leader + g.n ? (tokens >> a.log_p << a.log_p) / kPagedTile : 0;
+    return g;
+}
+__device__ __forceinline__ SharedRange shared_range(const PagedArgs& a, int e, int& kv) {
+    SharedRange r{0, 0, 0, 0, 0};
+    kv = 0;
+    if (e >= 2 * a.B) return r;
+    r.b = e < a.B ? e : e - a.B;
+    const Group g = group_of(a, r.b);
+    const int n = e >= a.B ? 1 : g.leader == r.b && g.tiles > 0 ? g.n : 0;
+    r.first = clamp_int(a.q_starts[r.b], 0, a.T);
+    r.len = clamp_int(a.q_starts[r.b + n], r.first, a.T) - r.first;
+    kv = clamp_int(a.kv_lens[r.b], 0, a.C << a.log_p);
+    r.tile = e < a.B ? 0 : g.tiles;
+    r.end = e < a.B ? g.tiles : kWholeAxis;
+    return r;
+}
+// the first of n ascending values that is above v, the same v in every lane; n if there is none
+__device__ __forceinline__ int first_above(const int32_t* values, int n, int v) {
+    const int lane = threadIdx.x & 63;
+    int at = 0;
+    if (n > 64) {
+        const int each = (n + 63) / 64;
+        const uint64_t above = __ballot(values[min((lane + 1) * each, n) - 1] > v);
+        if (above == 0) return n;
+        at = __builtin_ctzll(above) * each;
+    }
+    for (; at < n; at += 64) {
+        const uint64_t above = __ballot(at + lane < n && values[min(at + lane, n - 1)] > v);
+        if (above != 0) return at + __builtin_ctzll(above);
+    }
+    return n;
+}
+// position of the group's row `token`, found among its requests: where they bring as many tokens each, at the first try
+__device__ __forceinline__ int shared_position(const PagedArgs& a, const SharedRange& r, int members, int token) {
+    const int t = r.first + token;
+    int b = r.b + (int)((int64_t)token * members / r.len);
+    if (a.q_starts[b] > t || a.q_starts[b + 1] <= t) {
+        int lo = r.b, hi = r.b + members;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (a.q_starts[mid] <= t) lo = mid;
+            else hi = mid;
+        }
+        b = lo;
+    }
+    return clamp_int(a.kv_lens[b], 0, a.C << a.log_p) - clamp_int(a.q_starts[b + 1], 0, a.T) + t;
+}
+// What workgroup `item` of a part serves
+struct SharedUnit {
+    Share sh;
+    SharedRange range;
+    int members;                      // of the group whose common part it is; 0: the rest of a request
+    bool partial;
+};
+__device__ __forceinline__ SharedUnit shared_unit(const PagedArgs& a, const PagedPart& part, int item) {
+    SharedUnit u;
+    const int e = first_above(part.unit_end, 2 * a.B, item);
+    u.sh.b = -1;
+    if (e >= 2 * a.B) return u;
+    int kv;
+    u.range = shared_range(a, e, kv);
+    u.members = e < a.B ? group_of(a, u.range.b).n : 0;
+    u.sh.s = shared_share(part, a.G, u.range, e < a.B, kv, a.sink, a.window, *part.piece);
+    if (u.sh.s.tiles == 0) return u;
+    u.sh.b = u.range.b;
+    const int before = e > 0 ? part.unit_end[e - 1] : 0;
+    u.sh.unit = item - before;
+    u.sh.slot = before;
+    u.sh.r = Request{u.range.first, u.range.len, kv};
+    u.partial = u.range.tile > 0 || e < a.B || u.sh.s.splits > 1;
+    return u;
+}
+
 // a request's key tiles are dealt to its pieces evenly
 __device__ __forceinline__ int tiles_of_piece(const PagedShare& s) { return (int)((uint32_t)(s.keys + s.splits - 1) / (uint32_t)s.splits); }
 
@@ -268,7 +357,7 @@ __device__ __forceinline__ float sum_over_groups(float v) { v += __shfl_xor(v, 1
 // LDS of a workgroup: the wavefronts' outputs, references and denominators
 template <int D, int MF, int NW, int NV>
 constexpr int kFewLds = NW * 16 * (D / NV + 4) * 4 + 2 * NW * MF * 16 * 4;
-template <int D, int MF, bool MOD, int NP, int NW, int NV, bool Q8>
+template <int D, int MF, bool MOD, int NP, int NW, int NV, bool Q8, bool SHARED>
 __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& part, unsigned wg, unsigned units, char* lds) {
     constexpr int DS = D / 32;        // MFMAs of a logits tile
     constexpr int DV = D / NV;        // dims of the outputs
@@ -287,9 +376,17 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
     float (*const s_l)[MF * 16] = s_m + NW;
 
     const int dv0 = NV > 1 ? (int)(wg / units) * DV : 0;     // parts of a unit on one XCD where units are a multiple of 8
-    const Request first = request_at(a, threadIdx.x & 63);
-    const int piece = part_piece<false>(a, part, first, threadIdx.x & 63);
-    const Share sh = share_of<false>(a, part, piece, first, NV > 1 ? wg % units : wg);
+    Share sh;
+    [[maybe_unused]] SharedUnit unit;
+    if constexpr (SHARED) {
+        static_assert(NV == 1, "results of a unit lie in one place");
+        unit = shared_unit(a, part, (int)wg);
+        sh = unit.sh;
+    } else {
+        const Request first = request_at(a, threadIdx.x & 63);
+        const int piece = part_piece<false>(a, part, first, threadIdx.x & 63);
+        sh = share_of<false>(a, part, piece, first, NV > 1 ? wg % units : wg);
+    }
     if (sh.b < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4;
@@ -297,22 +394,47 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
     const int rows = sh.r.len * a.G, row0 = tile * part.m;
     const int last_row = min(row0 + part.m, rows) - 1;
     const int pos0 = sh.r.kv - sh.r.len;                        // position of the request's first new token
-    const int pos_lo = pos0 + row0 / a.G, pos_hi = pos0 + last_row / a.G;
-    const KeyTiles kt = key_tiles(pos_lo, pos_hi, a.sink, a.window);
+    int pos[MF];
+    int pos_lo = pos0 + row0 / a.G, pos_hi = pos0 + last_row / a.G;
+#pragma unroll
+    for (int f = 0; f < MF; ++f) pos[f] = pos0 + min(row0 + 16 * f + n16, last_row) / a.G;
+    if constexpr (SHARED) {
+        if (unit.members > 0) {                                 // rows of several requests
+            int lo = 0x7fffffff, hi = -0x7fffffff;
+#pragma unroll
+            for (int f = 0; f < MF; ++f) {
+                pos[f] = shared_position(a, unit.range, unit.members, min(row0 + 16 * f + n16, last_row) / a.G);
+                lo = min(lo, pos[f]);
+                hi = max(hi, pos[f]);
+            }
+#pragma unroll
+            for (int x = 1; x < 16; x <<= 1) {
+                lo = min(lo, __shfl_xor(lo, x));
+                hi = max(hi, __shfl_xor(hi, x));
+            }
+            pos_lo = __builtin_amdgcn_readfirstlane(lo);
+            pos_hi = __builtin_amdgcn_readfirstlane(hi);
+        }
+    }
+    const auto kt = [&] {
+        if constexpr (SHARED) return key_tiles_within(pos_lo, pos_hi, a.sink, a.window, unit.range.tile, unit.range.end);
+        else return key_tiles(pos_lo, pos_hi, a.sink, a.window);
+    }();
     const int per = tiles_of_piece(sh.s);
     const int e_end = min((cut + 1) * per, kt.n);               // of the row tile's key tiles
-    const int last_col = pos_hi >= 0 ? pos_hi >> a.log_p : 0;
+    const bool to_last = e_end == kt.n && (!SHARED || kt.n == 0 || kt.at(kt.n - 1) == pos_hi / kPagedTile);      // the tile of pos_hi is the last one
+    const int last_key = !SHARED || unit.range.end > pos_hi / kPagedTile ? pos_hi : unit.range.end * kPagedTile - 1;
+    const int last_col = last_key >= 0 ? last_key >> a.log_p : 0;
     const int page = 1 << a.log_p;
 
     bf16x8 qf[MF][DS];
-    int pos[MF], head[MF], token[MF];
+    int head[MF], token[MF];
     Logits lg[MF];
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
         const int row = min(row0 + 16 * f + n16, last_row);      // rows past the last repeat it; they are not stored
         token[f] = row / a.G;
         head[f] = kvh * a.G + row % a.G;
-        pos[f] = pos0 + token[f];
         const uint16_t* qrow = a.q + (int64_t)(sh.r.first + token[f]) * a.q_t + head[f] * a.q_h;
 #pragma unroll
         for (int s = 0; s < DS; ++s) qf[f][s] = *reinterpret_cast<const bf16x8*>(qrow + (Q8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g));
@@ -330,7 +452,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
     const int32_t* const trow = a.table + (int64_t)sh.b * a.table_stride;
     auto page_of = [&](int key) { return clamp_int(trow[min(key >> a.log_p, last_col)], 0, a.n_pages - 1); };
     // chunks of this workgroup: the last tile's second half only if a row sees it
-    const int c_end = CPT == 2 && e_end == kt.n && (pos_hi & (kPagedTile - 1)) < 32 ? 2 * e_end - 1 : CPT * e_end;
+    const int c_end = CPT == 2 && to_last && (pos_hi & (kPagedTile - 1)) < 32 ? 2 * e_end - 1 : CPT * e_end;
     auto key_of = [&](int c) { return CPT == 2 ? kt.at(c >> 1) * kPagedTile + 32 * (c & 1) : kt.at(c) * kPagedTile; };
     struct Pages {                                              // small pages: a chunk lies in NP of them
         int id[NP == 1 ? 1 : 2];                                // Q8: those that this lane's K rows and its values are in, else both
@@ -626,7 +748,8 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
         const float lq = sum_over_groups(l[f]);
         if (g == 0) { s_m[wave][16 * f + n16] = m[f]; s_l[wave][16 * f + n16] = lq; }
     }
-    const bool partial = sh.s.splits > 1;
+    bool partial = sh.s.splits > 1;
+    if constexpr (SHARED) partial = unit.partial;
     const int slot = sh.slot + sh.unit;
     if (partial && (unsigned)slot >= (unsigned)part.n_slots) return;                // starts that are not ascending: more units than there is room for
 #pragma unroll
@@ -676,10 +799,10 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
 }
 
 // NP: pages that a chunk of keys lies in
-template <int D, int MF, bool MOD, int NP, int NW, int NV, bool Q8>
+template <int D, int MF, bool MOD, int NP, int NW, int NV, bool Q8, bool SHARED>
 __global__ __launch_bounds__(64 * NW, MF > 1 || (Q8 && D == 128 && (NP > 1 || MOD)) ? 2 : D == 64 ? (Q8 ? 4 : 5) : 3) void paged_few_kernel(PagedArgs a, PagedPart part, unsigned units) {
     __shared__ __attribute__((aligned(16))) char lds[kFewLds<D, MF, NW, NV>];
-    few_rows<D, MF, MOD, NP, NW, NV, Q8>(a, part, blockIdx.x, units, lds);
+    few_rows<D, MF, MOD, NP, NW, NV, Q8, SHARED>(a, part, blockIdx.x, units, lds);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -788,7 +911,7 @@ __device__ __forceinline__ void lds_dma16_from(uint32_t lds_addr, const void* la
 // this wavefront's direct loads have landed
 __device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-template <int D, int MODE, bool SMALL, bool Q8>
+template <int D, int MODE, bool SMALL, bool Q8, bool SHARED>
 __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& part, unsigned wg, char* lds) {
     constexpr int NW = 4;
     constexpr int KT = kPagedTile;
@@ -806,10 +929,17 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     uint16_t (*const smemK)[TILE] = reinterpret_cast<uint16_t (*)[TILE]>(lds);      // K tile t in buffer t % 2
     uint16_t (*const smemV)[TILE] = smemK + 2;                                      // V^T likewise
 
-    const Request first = request_at(a, threadIdx.x & 63);
-    const int piece = part_piece<true>(a, part, first, threadIdx.x & 63);
-    if (part.n_slots > 0 && wg == 0 && threadIdx.x == 0) *part.piece = piece;
-    const Share sh = share_of<false>(a, part, piece, first, wg);
+    Share sh;
+    [[maybe_unused]] SharedUnit unit;
+    if constexpr (SHARED) {
+        unit = shared_unit(a, part, (int)wg);
+        sh = unit.sh;
+    } else {
+        const Request first = request_at(a, threadIdx.x & 63);
+        const int piece = part_piece<true>(a, part, first, threadIdx.x & 63);
+        if (part.n_slots > 0 && wg == 0 && threadIdx.x == 0) *part.piece = piece;
+        sh = share_of<false>(a, part, piece, first, wg);
+    }
     if (sh.b < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, l32 = lane & 31;
@@ -817,18 +947,45 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     const int rows = sh.r.len * a.G, row0 = tile * kManyRows;
     const int last_row = min(row0 + kManyRows, rows) - 1;
     const int pos0 = sh.r.kv - sh.r.len;
-    const int pos_lo = pos0 + row0 / a.G, pos_hi = pos0 + last_row / a.G;      // of the workgroup's rows
-    const KeyTiles kt = key_tiles(pos_lo, pos_hi, a.sink, a.window);
+    int pos_lo = pos0 + row0 / a.G, pos_hi = pos0 + last_row / a.G;            // of the workgroup's rows
+    const int row = min(row0 + 32 * wave + l32, last_row);                    // rows past the last repeat it; they are not stored
+    int pos = pos0 + row / a.G;
+    const int wave_row = row0 + 32 * wave;                                    // wave-uniform bounds of this wavefront's rows
+    int wave_lo = pos0 + min(wave_row, last_row) / a.G, wave_hi = pos0 + min(wave_row + 31, last_row) / a.G;
+    if constexpr (SHARED) {
+        if (unit.members > 0) {                                               // rows of several requests: a lane finds two of the 128
+            const int p0 = shared_position(a, unit.range, unit.members, min(row0 + lane, last_row) / a.G);
+            const int p1 = shared_position(a, unit.range, unit.members, min(row0 + 64 + lane, last_row) / a.G);
+            const int from = 32 * (wave & 1) + l32, q0 = __shfl(p0, from), q1 = __shfl(p1, from);
+            pos = wave < 2 ? q0 : q1;
+            int lo = pos, hi = pos, lo_all = min(p0, p1), hi_all = max(p0, p1);
+#pragma unroll
+            for (int x = 1; x < 64; x <<= 1) {
+                lo = min(lo, __shfl_xor(lo, x));
+                hi = max(hi, __shfl_xor(hi, x));
+                lo_all = min(lo_all, __shfl_xor(lo_all, x));
+                hi_all = max(hi_all, __shfl_xor(hi_all, x));
+            }
+            wave_lo = __builtin_amdgcn_readfirstlane(lo);
+            wave_hi = __builtin_amdgcn_readfirstlane(hi);
+            pos_lo = __builtin_amdgcn_readfirstlane(lo_all);
+            pos_hi = __builtin_amdgcn_readfirstlane(hi_all);
+        }
+    }
+    const auto kt = [&] {
+        if constexpr (SHARED) return key_tiles_within(pos_lo, pos_hi, a.sink, a.window, unit.range.tile, unit.range.end);
+        else return key_tiles(pos_lo, pos_hi, a.sink, a.window);
+    }();
     const int per = tiles_of_piece(sh.s);
     const int e0 = cut * per;
     const int n_st = min((cut + 1) * per, kt.n) - e0;                         // key tiles of this workgroup
-    const bool partial = sh.s.splits > 1;
+    bool partial = sh.s.splits > 1;
+    if constexpr (SHARED) partial = unit.partial;
     const int slot = sh.slot + sh.unit;
     if (partial && (unsigned)slot >= (unsigned)part.n_slots) return;
 
-    const int row = min(row0 + 32 * wave + l32, last_row);                    // rows past the last repeat it; they are not stored
     const bool valid = row0 + 32 * wave + l32 <= last_row;
-    const int token = row / a.G, head = kvh * a.G + row % a.G, pos = pos0 + token;
+    const int token = row / a.G, head = kvh * a.G + row % a.G;
     auto store_lse = [&](int at, float lse2) {                                // at: the row, counted from the workgroup's first
         if (partial) {
             part.lse[(int64_t)slot * kManyRows + at] = lse2;
@@ -853,7 +1010,8 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         return;
     }
 
-    const int last_col = pos_hi >> a.log_p;
+    const int last_key = !SHARED || unit.range.end > pos_hi / kPagedTile ? pos_hi : unit.range.end * kPagedTile - 1;
+    const int last_col = last_key >> a.log_p;
     const int page = 1 << a.log_p;
     const int32_t* const trow = a.table + (int64_t)sh.b * a.table_stride;
     using Value = PageValue<Q8>;
@@ -862,13 +1020,18 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     auto key_of = [&](int t) { return kt.at(kt.n - 1 - e0 - t) * KT; };       // first key of tile t: the last tiles first
     auto page_of = [&](int key) { return clamp_int(trow[min(key >> a.log_p, last_col)], 0, a.n_pages - 1); };
     struct Pages {                                                            // of a tile's 16-key pieces (one page without SMALL)
-        int id[SMALL ? 4 : 1];
+        int id[!SMALL ? 1 : Q8 ? 2 : 4];                                      // Q8: of the wavefront's keys, and of the lane's values
     };
     auto pages_of = [&](int t) {
         Pages p;
         const int key0 = key_of(min(t, n_st - 1));
+        if constexpr (SMALL && Q8) {
+            p.id[0] = page_of(key0 + 16 * wave);
+            p.id[1] = page_of(key0 + 16 * (lane & 3));
+        } else {
 #pragma unroll
-        for (int x = 0; x < (SMALL ? 4 : 1); ++x) p.id[x] = page_of(key0 + 16 * x);
+            for (int x = 0; x < (SMALL ? 4 : 1); ++x) p.id[x] = page_of(key0 + 16 * x);
+        }
         return p;
     };
 
@@ -951,9 +1114,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     };
     auto load_k = [&](int t, const Pages& pg, Raw& raw) {
         const int ln = lane_anew();
-        const int key = key_of(t) + 16 * wave;
-        int id = pg.id[0];
-        if constexpr (SMALL) id = __builtin_amdgcn_readfirstlane(wave == 0 ? pg.id[0] : wave == 1 ? pg.id[1] : wave == 2 ? pg.id[2] : pg.id[3]);
+        const int key = key_of(t) + 16 * wave, id = pg.id[0];
         const char* const src = kbase + ((int64_t)id * a.kp_p + (key & (page - 1)) * D);
         const uint8_t* const exps = a.exps.k + id * a.exps.k_p + kvh * a.exps.k_h + (key & (page - 1));
 #pragma unroll
@@ -966,8 +1127,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     auto load_v = [&](int t, const Pages& pg, Raw& raw) {
         const int ln = lane_anew();
         const int key = key_of(t) + 16 * (ln & 3);
-        int id = pg.id[0];
-        if constexpr (SMALL) id = (ln & 3) == 0 ? pg.id[0] : (ln & 3) == 1 ? pg.id[1] : (ln & 3) == 2 ? pg.id[2] : pg.id[3];
+        const int id = pg.id[SMALL ? 1 : 0];
         const char* const src = vbase0 + ((int64_t)id * a.vp_p + (key & (page - 1)));
         raw.v_exp = *reinterpret_cast<const u32x4*>(a.exps.v + id * a.exps.v_p + kvh * a.exps.v_h + (key & (page - 1)));
 #pragma unroll
@@ -1110,8 +1270,6 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     cw.k = ChunkWeights<MODE>::kCap ? fminf(2.f * cw.c / a.cap, 3e38f) : 0.f;     // finite, so that a product of 0 stays 0
     cw.slope2 = ChunkWeights<MODE>::kBias ? a.slopes[head] * kLog2e : 0.f;
     float m = 0.f, l = INFINITY;
-    const int wave_row = row0 + 32 * wave;                                    // wave-uniform bounds of this wavefront's rows
-    const int wave_lo = pos0 + min(wave_row, last_row) / a.G, wave_hi = pos0 + min(wave_row + 31, last_row) / a.G;
     auto needs_mask = [&](int key0) { return hides(a, wave_lo, wave_hi, key0, 32); };
     // Slow path of a chunk: masks, and a reference that makes its weights at most 1 and the denominator so far about 1 or less.
     // For the first chunk, masked ones, and where the denominator passed the limit.
@@ -1311,23 +1469,89 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
 constexpr int pages_of_chunk(int pages, bool q8) { return q8 ? 1 << pages : pages == 2 ? 2 : 1; }
 // PAGES: 2, pages of 16 tokens; 1, of 32; 0, a key tile lies in one page.  With head_dim 64 and a key tile in one page three wavefronts share
 // a SIMD (prompts of 4000 tokens with slopes 228 -> 197 us); cap and slopes together do not leave the registers for it.
-template <int D, int MODE, int PAGES, bool Q8>
+template <int D, int MODE, int PAGES, bool Q8, bool SHARED>
 __global__ __launch_bounds__(256, D == 64 && PAGES == 0 && MODE != kCappedSlopes && !Q8 ? 3 : 2) void paged_attn_kernel(PagedArgs a, PagedPart many, unsigned many_grid, PagedPart few) {
     __shared__ __attribute__((aligned(1024))) char lds[4 * kPagedTile * D * 2];
     static_assert(kFewLds<D, 1, 4, 1> <= 4 * kPagedTile * D * 2, "few rows fit the tile buffers");
-    if (blockIdx.x < many_grid) many_rows<D, MODE, PAGES != 0, Q8>(a, many, blockIdx.x, lds);
-    else few_rows<D, 1, MODE != kPlain, pages_of_chunk(PAGES, Q8), 4, 1, Q8>(a, few, blockIdx.x - many_grid, 0, lds);
+    if (blockIdx.x < many_grid) many_rows<D, MODE, PAGES != 0, Q8, SHARED>(a, many, blockIdx.x, lds);
+    else few_rows<D, 1, MODE != kPlain, pages_of_chunk(PAGES, Q8), 4, 1, Q8, SHARED>(a, few, blockIdx.x - many_grid, 0, lds);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
 // Merge of the pieces' results: out = sum_s w_s out_s / sum_s w_s, w_s = 2^(lse_s - max).  A wavefront makes D / NV dims of a row, 64 pieces
 // at a time: a lane has the weight of one, then DV / 4 lanes read a piece's values, 64 / (DV / 4) pieces side by side.  NV = 4 for few
 // rows: what a CU takes in bounds them (4 requests behind 128K tokens, 128 rows of 64 pieces: 11.7 -> 7.6 us).
+struct PieceSums {
+    float mx = -INFINITY, total = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+};
+// adds the pieces slot0, slot0 + step, .. of row rt of a part's row tile: dims d0 .. + 3 of a lane
+template <int D, int NV>
+__device__ __forceinline__ void add_pieces(const PagedPart& part, int slot0, int step, int splits, int rt, int d0, PieceSums& sums) {
+    constexpr int DV = D / NV, LPR = DV / 4, NG = 64 / LPR;       // dims of a wavefront, lanes of a piece, pieces side by side
+    const int lane = threadIdx.x & 63, grp = lane / LPR;
+    auto at = [&](int s) { return (int64_t)(slot0 + s * step) * part.m + rt; };
+    float mx = sums.mx, total = sums.total;
+    f32x4 acc = sums.acc;
+    for (int s0 = 0; s0 < splits; s0 += 64) {
+        const float v = s0 + lane < splits ? part.lse[at(s0 + lane)] : -INFINITY;
+        float top = v;
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));     // NaN is dropped here and comes back with the weights
+        const float mx_new = fmaxf(mx, top);
+        const float old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - mx_new);
+        mx = mx_new;
+        const float w = v == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(v - mx);
+        const uint64_t with_keys = __ballot(v != -INFINITY);    // of weight 0, too: the piece may hold an infinite or NaN value
+        total = fmaf(total, old, w);
+        acc *= old;
+        const int n = min(64, splits - s0);
+        for (int s = 0; s < n; s += 4 * NG) {           // four loads of a lane in flight
+            float ws[4];
+            bool some[4];
+            f32x4 p[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int mine = s + NG * y + grp, there = min(mine, n - 1);
+                ws[y] = __shfl(w, there);
+                some[y] = mine < n && (with_keys >> there & 1) != 0;
+                p[y] = *reinterpret_cast<const f32x4*>(part.o + at(s0 + there) * D + d0);
+            }
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)             // a piece without a key in sight may not have written its values
+                    acc[x] = some[y] ? fmaf(p[y][x], ws[y], acc[x]) : acc[x];
+        }
+    }
+    sums.mx = mx;
+    sums.total = total;
+    sums.acc = acc;
+}
+// the lanes' sums become a row's output
+template <int D, int NV>
+__device__ __forceinline__ void finish_row(const PagedArgs& a, const PieceSums& sums, int tok, int hd, int pos, int d0) {
+    constexpr int LPR = D / NV / 4;
+    const int lane = threadIdx.x & 63;
+    float total = sums.total;
+    f32x4 acc = sums.acc;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) total += __shfl_xor(total, x);
+#pragma unroll
+    for (int x = LPR; x < 64; x <<= 1)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) acc[y] += __shfl_xor(acc[y], x);
+    const bool none = total == 0.f || (sums.mx <= kNoLogit && total == total);       // NaN is not none
+    const float inv = none ? without_logits(pos) : 1.f / total;
+    if (lane < LPR) {
+        *reinterpret_cast<bf16x4*>(a.out + (int64_t)tok * a.o_t + hd * a.o_h + d0) = __builtin_convertvector(acc * inv, bf16x4);
+        if (a.lse != nullptr && lane == 0 && d0 == 0) a.lse[(int64_t)tok * a.Hq + hd] = none ? -INFINITY : (sums.mx + __log2f(total)) * kLn2;
+    }
+}
 template <int D, int NV, bool MANY>
 __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& part) {
-    constexpr int DV = D / NV, LPR = DV / 4, NG = 64 / LPR;       // dims of a wavefront, lanes of a piece, pieces side by side
+    constexpr int DV = D / NV, LPR = DV / 4;
     const int lane = threadIdx.x & 63;
-    const int grp = lane / LPR;
     const Request first = request_at(a, lane);
     // found anew, or, where that takes longer than a load, as the attention kernel has left it
     const int piece = MANY ? __builtin_amdgcn_readfirstlane(*part.piece) : part_piece<false>(a, part, first, lane);
@@ -1340,53 +1564,9 @@ __device__ __forceinline__ void merge_rows(const PagedArgs& a, const PagedPart& 
         const int tile = row >> part.log_m, rt = row & (part.m - 1);
         const int slot0 = sh.slot + (sh.s.tiles - 1 - tile) * splits * a.Hkv + kvh;
         if (slot0 < 0 || slot0 + (splits - 1) * a.Hkv >= part.n_slots) continue;
-        auto at = [&](int s) { return (int64_t)(slot0 + s * a.Hkv) * part.m + rt; };
-        float mx = -INFINITY, total = 0.f;
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int s0 = 0; s0 < splits; s0 += 64) {
-            const float v = s0 + lane < splits ? part.lse[at(s0 + lane)] : -INFINITY;
-            float top = v;
-#pragma unroll
-            for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));     // NaN is dropped here and comes back with the weights
-            const float mx_new = fmaxf(mx, top);
-            const float old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - mx_new);
-            mx = mx_new;
-            const float w = v == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(v - mx);
-            const uint64_t with_keys = __ballot(v != -INFINITY);    // of weight 0, too: the piece may hold an infinite or NaN value
-            total = fmaf(total, old, w);
-            acc *= old;
-            const int n = min(64, splits - s0);
-            for (int s = 0; s < n; s += 4 * NG) {           // four loads of a lane in flight
-                float ws[4];
-                bool some[4];
-                f32x4 p[4];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const int mine = s + NG * y + grp, there = min(mine, n - 1);
-                    ws[y] = __shfl(w, there);
-                    some[y] = mine < n && (with_keys >> there & 1) != 0;
-                    p[y] = *reinterpret_cast<const f32x4*>(part.o + at(s0 + there) * D + d0);
-                }
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)             // a piece without a key in sight may not have written its values
-                        acc[x] = some[y] ? fmaf(p[y][x], ws[y], acc[x]) : acc[x];
-            }
-        }
-#pragma unroll
-        for (int x = 1; x < 64; x <<= 1) total += __shfl_xor(total, x);
-#pragma unroll
-        for (int x = LPR; x < 64; x <<= 1)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) acc[y] += __shfl_xor(acc[y], x);
-        const bool none = total == 0.f || (mx <= kNoLogit && total == total);       // NaN is not none
-        const float inv = none ? without_logits(sh.r.kv - sh.r.len + row / a.G) : 1.f / total;
-        if (lane < LPR) {
-            const int tok = sh.r.first + row / a.G, hd = kvh * a.G + row % a.G;
-            *reinterpret_cast<bf16x4*>(a.out + (int64_t)tok * a.o_t + hd * a.o_h + d0) = __builtin_convertvector(acc * inv, bf16x4);
-            if (a.lse != nullptr && lane == 0 && d0 == 0) a.lse[(int64_t)tok * a.Hq + hd] = none ? -INFINITY : (mx + __log2f(total)) * kLn2;
-        }
+        PieceSums sums;
+        add_pieces<D, NV>(part, slot0, a.Hkv, splits, rt, d0, sums);
+        finish_row<D, NV>(a, sums, sh.r.first + row / a.G, kvh * a.G + row % a.G, sh.r.kv - sh.r.len + row / a.G, d0);
     }
 }
 template <int D, int NV>
@@ -1416,18 +1596,36 @@ int64_t most_slots(const PagedDims& d, const PagedPart& part) {
     return units < most ? units : most;
 }
 
-template <int D, int MF, int NW, int NV, bool Q8>
+template <int D, int MF, int NW, int NV, bool Q8, bool SHARED>
 void launch_few(const PagedArgs& a, const PagedPart& part, unsigned units, hipStream_t st) {
     const bool mod = a.cap > 0.f || a.slopes != nullptr;
     const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(units * NV), dim3(64 * NW), 0, st, a, part, units); };
     const auto with_pages = [&](auto np) {
         constexpr int NP = decltype(np)::value;
-        if (mod) go(paged_few_kernel<D, MF, true, NP, NW, NV, Q8>);
-        else go(paged_few_kernel<D, MF, false, NP, NW, NV, Q8>);
+        if (mod) go(paged_few_kernel<D, MF, true, NP, NW, NV, Q8, SHARED>);
+        else go(paged_few_kernel<D, MF, false, NP, NW, NV, Q8, SHARED>);
     };
     if (a.log_p == 4) with_pages(IC<pages_of_chunk(2, Q8)>{});
     else if (Q8 && a.log_p == 5) with_pages(IC<pages_of_chunk(1, Q8)>{});
     else with_pages(IC<1>{});
+}
+
+// Requests of many rows, and of few ones behind them (few_grid workgroups)
+template <int D, bool Q8, bool SHARED>
+void launch_many(const PagedArgs& a, const PagedParts& parts, int64_t many_grid, int64_t few_grid, hipStream_t st) {
+    const auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(many_grid + few_grid)), dim3(256), 0, st, a, parts.many, (unsigned)many_grid, parts.few);
+    };
+    const auto with_pages = [&](auto mode) {
+        constexpr int MODE = decltype(mode)::value;
+        if (a.log_p == 4) go(paged_attn_kernel<D, MODE, 2, Q8, SHARED>);
+        else if (a.log_p == 5) go(paged_attn_kernel<D, MODE, 1, Q8, SHARED>);
+        else go(paged_attn_kernel<D, MODE, 0, Q8, SHARED>);
+    };
+    if (a.cap > 0.f && a.slopes != nullptr) with_pages(IC<kCappedSlopes>{});
+    else if (a.cap > 0.f) with_pages(IC<kCapped>{});
+    else if (a.slopes != nullptr) with_pages(IC<kSlopes>{});
+    else with_pages(IC<kPlain>{});
 }
 
 template <int D, bool Q8>
@@ -1438,26 +1636,14 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
     const int64_t few_grid = parts.few.m ? most_units(d, parts.few) : 0, many_grid = parts.many.m ? most_units(d, parts.many) : 0;
     if (few_grid + many_grid > 0x7fffffffll) return hipErrorInvalidValue;
     if (parts.few.m && !both) {
-        if (parts.few.m == 32) launch_few<D, 2, 4, 1, Q8>(a, parts.few, (unsigned)few_grid, st);
-        else if (few_grid <= 64) launch_few<D, 1, 8, 4, Q8>(a, parts.few, (unsigned)few_grid, st);
-        else launch_few<D, 1, 4, 1, Q8>(a, parts.few, (unsigned)few_grid, st);
+        if (parts.few.m == 32) launch_few<D, 2, 4, 1, Q8, false>(a, parts.few, (unsigned)few_grid, st);
+        else if (few_grid <= 64) launch_few<D, 1, 8, 4, Q8, false>(a, parts.few, (unsigned)few_grid, st);
+        else launch_few<D, 1, 4, 1, Q8, false>(a, parts.few, (unsigned)few_grid, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (parts.many.m) {
-        const auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(many_grid + (both ? few_grid : 0))), dim3(256), 0, st, a, parts.many, (unsigned)many_grid, parts.few);
-        };
-        const auto with_pages = [&](auto mode) {
-            constexpr int MODE = decltype(mode)::value;
-            if (a.log_p == 4) go(paged_attn_kernel<D, MODE, 2, Q8>);
-            else if (a.log_p == 5) go(paged_attn_kernel<D, MODE, 1, Q8>);
-            else go(paged_attn_kernel<D, MODE, 0, Q8>);
-        };
-        if (a.cap > 0.f && a.slopes != nullptr) with_pages(IC<kCappedSlopes>{});
-        else if (a.cap > 0.f) with_pages(IC<kCapped>{});
-        else if (a.slopes != nullptr) with_pages(IC<kSlopes>{});
-        else with_pages(IC<kPlain>{});
+        launch_many<D, Q8, false>(a, parts, many_grid, both ? few_grid : 0, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -1468,11 +1654,25 @@ hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts
     return hipGetLastError();
 }
 
+// The attention kernels of a call with shared prompts, between the one that cuts it and the merge
+template <int D, bool Q8>
+hipError_t launch_shared_parts(const PagedArgs& a, const PagedParts& parts, hipStream_t st) {
+    const bool apart = parts.few.m == 32;             // 17 to 32 query heads of a KV head: one after the other, as in launch_parts
+    if (apart) {
+        launch_few<D, 2, 4, 1, Q8, true>(a, parts.few, (unsigned)parts.few.n_slots, st);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    launch_many<D, Q8, true>(a, parts, parts.many.n_slots, apart ? 0 : parts.few.n_slots, st);
+    return hipGetLastError();
+}
+
 PagedArgs paged_args(const PagedDims& d, const void* q, const void* k_pages, const void* vt_pages, const PagedExps& exps, const int32_t* block_table,
-                     const int32_t* q_starts, const int32_t* kv_lens, const float* slopes_or_null, void* out, float* lse_or_null) {
+                     const int32_t* q_starts, const int32_t* kv_lens, const int32_t* shares_or_null, const float* slopes_or_null, void* out,
+                     float* lse_or_null) {
     return {(const uint16_t*)q, k_pages, vt_pages, block_table, q_starts, kv_lens, slopes_or_null,
             (uint16_t*)out, lse_or_null, d.B, d.Hq, d.Hkv, d.G, d.T, d.log_p, d.n_pages, d.C, d.sink, d.window, d.scale, d.cap,
-            d.table_stride, d.q_t, d.q_h, d.o_t, d.o_h, d.kp_p, d.kp_h, d.vp_p, d.vp_h, exps};
+            d.table_stride, d.q_t, d.q_h, d.o_t, d.o_h, d.kp_p, d.kp_h, d.vp_p, d.vp_h, exps, shares_or_null};
 }
 
 }  // namespace

@@ -119,96 +119,6 @@ __global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a) {
     *reinterpret_cast<uint4*>(a.v + t * a.v_t + h * a.v_h + 8 * c) = vr;
 }
 
-// Attention in the plainest way: a wavefront for each query and head, 64 keys at a time, a key to a lane for the logits and dims to a
-// lane for the values.
-struct PlainArgs {
-    const uint16_t* q;
-    const void *k, *vt;
-    PagedExps exps;
-    const int32_t *table, *q_starts, *kv_lens;
-    const float* slopes;
-    uint16_t* out;
-    float* lse;
-    PagedDims d;
-};
-template <int D, bool Q8>
-__global__ __launch_bounds__(64) void paged_plain_kernel(PlainArgs a) {
-    constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-    __shared__ float s_q[D];
-    const int lane = threadIdx.x, t = blockIdx.x, head = blockIdx.y, h = head / a.d.G;
-    int lo = 0, hi = a.d.B;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.q_starts[mid] <= t) lo = mid;
-        else hi = mid;
-    }
-    const int first = a.q_starts[lo], end = a.q_starts[lo + 1];
-    if (t < first || t >= end) return;
-    const int64_t pos = (int64_t)clamp_int(a.kv_lens[lo], 0, a.d.C << a.d.log_p) - end + t;
-    for (int d = lane; d < D; d += 64) s_q[d] = __uint_as_float((uint32_t)a.q[t * a.d.q_t + head * a.d.q_h + d] << 16);
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, o[D / 64];
-    for (int x = 0; x < D / 64; ++x) o[x] = 0.f;
-    const int page = 1 << a.d.log_p;
-    for (int64_t key0 = 0; key0 <= pos; key0 += 64) {
-        if (a.d.window > 0 && key0 + 63 <= pos - a.d.window && key0 >= a.d.sink) continue;
-        const int64_t key = key0 + lane;
-        const bool seen = key <= pos && (a.d.window == 0 || pos - key < a.d.window || key < a.d.sink);
-        const int id = seen ? clamp_int(a.table[lo * a.d.table_stride + (key >> a.d.log_p)], 0, a.d.n_pages - 1) : 0;
-        const int in_page = (int)key & (page - 1);
-        float x = -INFINITY;
-        if (seen) {
-            float s = 0.f;
-            const int64_t at = id * a.d.kp_p + h * a.d.kp_h + in_page * D;
-            if constexpr (Q8) {
-                for (int d = 0; d < D; d += 4) {
-                    const uint32_t w = *reinterpret_cast<const uint32_t*>((const uint8_t*)a.k + at + d);
-                    const auto u = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), v = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-                    s += s_q[d] * u[0] + s_q[d + 1] * u[1] + s_q[d + 2] * v[0] + s_q[d + 3] * v[1];
-                }
-                s *= two_to(a.exps.k[id * a.exps.k_p + h * a.exps.k_h + in_page]);
-            } else {
-                for (int d = 0; d < D; d += 2) {
-                    const uint32_t w = *reinterpret_cast<const uint32_t*>((const uint16_t*)a.k + at + d);
-                    s += s_q[d] * bf16_lo(w) + s_q[d + 1] * bf16_hi(w);
-                }
-            }
-            x = s * a.d.scale;
-            if (a.d.cap > 0.f) x = a.d.cap * tanhf(x / a.d.cap);
-            if (a.slopes != nullptr) x -= a.slopes[head] * (float)(pos - key);
-            x *= kLog2e;
-        }
-        float mx = x;
-        for (int n = 1; n < 64; n <<= 1) mx = fmaxf(mx, __shfl_xor(mx, n));
-        const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = m == -INFINITY ? 0.f : exp2f(m - ref);
-        float w = seen ? exp2f(x - ref) : 0.f, sum = w;
-        for (int n = 1; n < 64; n <<= 1) sum += __shfl_xor(sum, n);
-        l = l * alpha + sum;
-        m = m_new;
-        if constexpr (Q8) w *= seen ? two_to(a.exps.v[id * a.exps.v_p + h * a.exps.v_h + in_page]) : 0.f;
-        const uint64_t some = __ballot(seen);
-        for (int y = 0; y < D / 64; ++y) o[y] *= alpha;
-        for (int j = 0; j < 64; ++j) {
-            if (!(some >> j & 1)) continue;
-            const float wj = __shfl(w, j);
-            const int64_t at = (int64_t)__shfl(id, j) * a.d.vp_p + h * a.d.vp_h + __shfl(in_page, j);
-            for (int y = 0; y < D / 64; ++y) {
-                const int64_t place = at + (int64_t)(lane + 64 * y) * page;
-                float value;
-                if constexpr (Q8) value = __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t*)a.vt)[place], 0);
-                else value = __uint_as_float((uint32_t)((const uint16_t*)a.vt)[place] << 16);
-                o[y] = fmaf(wj, value, o[y]);
-            }
-        }
-    }
-    const bool none = m == -INFINITY && l == 0.f;
-    const float inv = none ? (pos < 0 ? 0.f : NAN) : 1.f / l;
-    for (int y = 0; y < D / 64; ++y)
-        *reinterpret_cast<__bf16*>(a.out + t * a.d.o_t + head * a.d.o_h + lane + 64 * y) = (__bf16)(o[y] * inv);
-    if (a.lse != nullptr && lane == 0) a.lse[(int64_t)t * a.d.Hq + head] = none ? -INFINITY : (m + log2f(l)) * kLn2;
-}
-
 template <int D>
 hipError_t launch_append(const PagedDims& d, const void* k, int64_t k_t, int64_t k_h, const void* v, int64_t v_t, int64_t v_h,
                          const int32_t* slots, void* k_pages, void* vt_pages, const PagedExps& exps, hipStream_t st) {
@@ -237,17 +147,6 @@ hipError_t launch_paged_read(const PagedDims& d, const void* k_pages, const void
     const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)nwg), dim3(256), 0, st, a); };
     if (exps.k != nullptr) d.D == 128 ? go(paged_read_kernel<128, true>) : go(paged_read_kernel<64, true>);
     else d.D == 128 ? go(paged_read_kernel<128, false>) : go(paged_read_kernel<64, false>);
-    return hipGetLastError();
-}
-
-hipError_t launch_paged_plainly(const PagedDims& d, const void* q, const void* k_pages, const void* vt_pages, const PagedExps& exps,
-                                const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens, const float* slopes_or_null, void* out,
-                                float* lse_or_null, hipStream_t st) {
-    const PlainArgs a{(const uint16_t*)q, k_pages, vt_pages, exps, block_table, q_starts, kv_lens, slopes_or_null, (uint16_t*)out, lse_or_null, d};
-    if (d.Hq > 65535) return hipErrorInvalidValue;
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(d.T, d.Hq), dim3(64), 0, st, a); };
-    if (exps.k != nullptr) d.D == 128 ? go(paged_plain_kernel<128, true>) : go(paged_plain_kernel<64, true>);
-    else d.D == 128 ? go(paged_plain_kernel<128, false>) : go(paged_plain_kernel<64, false>);
     return hipGetLastError();
 }
 
