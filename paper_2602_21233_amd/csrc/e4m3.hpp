@@ -30,4 +30,26 @@ __device__ __forceinline__ uint32_t to_bf16_pair(uint32_t word, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, scale, HI));
 }
 
+// bytes of 8 rows of 8 the other way round
+__device__ __forceinline__ void transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t (&out)[4]) {
+    const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ab2 = __builtin_amdgcn_perm(b, a, 0x07030602u);
+    const uint32_t cd0 = __builtin_amdgcn_perm(d, c, 0x05010400u), cd2 = __builtin_amdgcn_perm(d, c, 0x07030602u);
+    out[0] = __builtin_amdgcn_perm(cd0, ab0, 0x05040100u);
+    out[1] = __builtin_amdgcn_perm(cd0, ab0, 0x07060302u);
+    out[2] = __builtin_amdgcn_perm(cd2, ab2, 0x05040100u);
+    out[3] = __builtin_amdgcn_perm(cd2, ab2, 0x07060302u);
+}
+__device__ __forceinline__ void transpose8(const uint2 (&in)[8], uint2 (&out)[8]) {
+    uint32_t t[4];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        transpose4(in[4 * x].x, in[4 * x + 1].x, in[4 * x + 2].x, in[4 * x + 3].x, t);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) (x ? out[y].y : out[y].x) = t[y];
+        transpose4(in[4 * x].y, in[4 * x + 1].y, in[4 * x + 2].y, in[4 * x + 3].y, t);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) (x ? out[4 + y].y : out[4 + y].x) = t[y];
+    }
+}
+
 }  // namespace spa
