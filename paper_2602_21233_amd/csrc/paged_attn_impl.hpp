@@ -1133,62 +1133,55 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
 #pragma unroll
         for (int x = 0; x < LQ; ++x) raw.v[x] = *reinterpret_cast<const u32x4*>(src + (16 * (wave * LQ + x) + (ln >> 2)) * page);
     };
-    auto stage_k = [&](auto buf_tag, const Raw& raw) {
-        constexpr int BUF = decltype(buf_tag)::value;
-        const int ln = lane_anew();
+    // where a lane's first 16 bytes go: the others are 8 keys (K, head_dim 128) or 16 dims further on, with a bit of the chunk turned
+    struct Places {
+        uint32_t k, v;
+        u32x4 w[LQ];                                          // values on their way
+    };
+    auto places = [&](Places& at) {
+        const int ln = lane_anew(), krow = 16 * wave + ln / CQ, vrow = 16 * wave * LQ + (ln >> 2);
+        at.k = 2 * (krow * D + (((2 * (ln % CQ)) ^ swz_k<D>(krow)) << 3));
+        at.v = 2 * (vrow * KT + (((2 * (ln & 3)) ^ swz_v(vrow)) << 3));
+    };
+    // part i of 2 LQ of K: 8 dims of a key
+    auto stage_k = [&](auto buf_tag, auto i_tag, const Raw& raw, const Places& at) __attribute__((always_inline)) {
+        constexpr int BUF = decltype(buf_tag)::value, x = decltype(i_tag)::value / 2, y = decltype(i_tag)::value % 2;
+        char* const to = reinterpret_cast<char*>(&smemK[BUF][0]) + ((at.k ^ (uint32_t)(16 * y + 32 * x)) + x * (64 / CQ) * D * 2);
+        *reinterpret_cast<bf16x8*>(to) = bf16_of(raw.k[x][2 * y], raw.k[x][2 * y + 1], two_to(raw.k_exp[x]));
+    };
+    // part i of 8 of V^T: a pair of keys for each of the lane's dims.  Their exponents differ: the pair converted with either, one half of each.
+    auto stage_v = [&](auto buf_tag, auto i_tag, const Raw& raw, Places& at) __attribute__((always_inline)) {
+        constexpr int BUF = decltype(buf_tag)::value, y = decltype(i_tag)::value / 4, z = decltype(i_tag)::value % 4;
+        constexpr int word = 2 * y + z / 2;
+        const float s0 = two_to(raw.v_exp[word] >> (16 * (z % 2)) & 0xffu), s1 = two_to(raw.v_exp[word] >> (16 * (z % 2) + 8) & 0xffu);
 #pragma unroll
         for (int x = 0; x < LQ; ++x) {
-            const int krow = 16 * wave + 64 / CQ * x + ln / CQ;
-            const float scale = two_to(raw.k_exp[x]);
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-                *reinterpret_cast<bf16x8*>(&smemK[BUF][krow * D + (((2 * (ln % CQ) + y) ^ swz_k<D>(krow)) << 3)]) = bf16_of(raw.k[x][2 * y], raw.k[x][2 * y + 1], scale);
+            const uint32_t lo = to_bf16_pair<z % 2 != 0>(raw.v[x][word], s0), hi = to_bf16_pair<z % 2 != 0>(raw.v[x][word], s1);
+            at.w[x][z] = (lo & 0xffffu) | (hi & 0xffff0000u);
+            if constexpr (z == 3) *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(&smemV[BUF][0]) + (at.v ^ (uint32_t)(16 * y)) + x * 16 * KT * 2) = at.w[x];
         }
     };
-    auto stage_v = [&](auto buf_tag, int t, Raw& raw) {
-        constexpr int BUF = decltype(buf_tag)::value;
-        const int ln = lane_anew();
-        const int key0 = key_of(t);
-        if (hides(a, pos_lo, pos_hi, key0, KT)) {             // as clear_unseen, with exponents that do no harm
-            bool odd = false;
+    // V^T of tile t where it is masked: as clear_unseen, with exponents that do no harm
+    auto mask_raw = [&](int t, Raw& raw) {
+        const int ln = lane_anew(), key0 = key_of(t);
+        if (!hides(a, pos_lo, pos_hi, key0, KT)) return;
+        bool odd = false;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const uint32_t keep = kept_bytes(key0 + 16 * (ln & 3) + 4 * y, pos_hi, a.sink, gone_hi);
-                raw.v_exp[y] = (raw.v_exp[y] & keep) | (0x7f7f7f7fu & ~keep);
+        for (int y = 0; y < 4; ++y) {
+            const uint32_t keep = kept_bytes(key0 + 16 * (ln & 3) + 4 * y, pos_hi, a.sink, gone_hi);
+            raw.v_exp[y] = (raw.v_exp[y] & keep) | (0x7f7f7f7fu & ~keep);
 #pragma unroll
-                for (int x = 0; x < LQ; ++x) {
-                    raw.v[x][y] &= keep;
-                    odd |= not_finite<true>(raw.v[x][y]);
-                }
-            }
-            if (__any(odd)) {
-                put_back = 1;
-#pragma unroll
-                for (int x = 0; x < LQ; ++x)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) raw.v[x][y] = finite_part<true>(raw.v[x][y]);
+            for (int x = 0; x < LQ; ++x) {
+                raw.v[x][y] &= keep;
+                odd |= not_finite<true>(raw.v[x][y]);
             }
         }
-        // the exponents of a pair's keys differ: the pair converted with either, one half of each
-        float scale[16];
+        if (__any(odd)) {
+            put_back = 1;
 #pragma unroll
-        for (int z = 0; z < 16; ++z) scale[z] = two_to(raw.v_exp[z / 4] >> (8 * (z % 4)) & 0xffu);
+            for (int x = 0; x < LQ; ++x)
 #pragma unroll
-        for (int x = 0; x < LQ; ++x) {
-            const int vrow = 16 * (wave * LQ + x) + (ln >> 2);
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                u32x4 w;
-#pragma unroll
-                for (int z = 0; z < 4; ++z) {
-                    const uint32_t from = raw.v[x][2 * y + z / 2];
-                    const float s0 = scale[8 * y + 2 * z], s1 = scale[8 * y + 2 * z + 1];
-                    const uint32_t lo = z % 2 ? to_bf16_pair<true>(from, s0) : to_bf16_pair<false>(from, s0);
-                    const uint32_t hi = z % 2 ? to_bf16_pair<true>(from, s1) : to_bf16_pair<false>(from, s1);
-                    w[z] = (lo & 0xffffu) | (hi & 0xffff0000u);
-                }
-                *reinterpret_cast<u32x4*>(&smemV[BUF][vrow * KT + (((2 * (ln & 3) + y) ^ swz_v(vrow)) << 3)]) = w;
-            }
+                for (int y = 0; y < 4; ++y) raw.v[x][y] = finite_part<true>(raw.v[x][y]);
         }
     };
     auto clear_unseen = [&](auto buf_tag, int t) {
@@ -1229,9 +1222,12 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         load_k(0, pg0, raw);
         load_v(0, pg0, raw);
         if (n_st > 1) load_k(1, pg1, next);
-        stage_k(IC<0>{}, raw);
-        stage_v(IC<0>{}, 0, raw);
-        if (n_st > 1) stage_k(IC<1>{}, next);
+        Places at;
+        places(at);
+        mask_raw(0, raw);
+        static_for<2 * LQ>([&](auto i_tag) { stage_k(IC<0>{}, i_tag, raw, at); });
+        static_for<8>([&](auto i_tag) { stage_v(IC<0>{}, i_tag, raw, at); });
+        if (n_st > 1) static_for<2 * LQ>([&](auto i_tag) { stage_k(IC<1>{}, i_tag, next, at); });
     } else {
         const Pages pg0 = pages_of(0);
         issue_k(IC<0>{}, 0, pg0);
@@ -1382,8 +1378,11 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         using VB = IC<PAR>;
         if (t > 0) {                                       // K(t + 1) and V^T(t) have been requested
             if constexpr (Q8) {                            // the buffers were last read before the barrier of tile t - 1
-                if (t + 1 < n_st) stage_k(KB{}, raw);
-                stage_v(VB{}, t, raw);
+                Places at;
+                places(at);
+                mask_raw(t, raw);
+                if (t + 1 < n_st) static_for<2 * LQ>([&](auto i_tag) { stage_k(KB{}, i_tag, raw, at); });
+                static_for<8>([&](auto i_tag) { stage_v(VB{}, i_tag, raw, at); });
             } else {
                 wait_for_loads();
                 clear_unseen(VB{}, t);

@@ -8,7 +8,7 @@
 namespace spa {
 namespace {
 
-constexpr int kCutThreads = 1024, kCutEach = 2 * kMaxRequests / kCutThreads;
+constexpr int kCutThreads = 1024;
 constexpr int64_t kMostUnits = 1 << 30;
 
 // sum or maximum over the workgroup, in every thread
@@ -22,29 +22,29 @@ __device__ __forceinline__ void over_workgroup(T (&v)[N], T (*s)[kCutThreads / 6
         if (lane == 0) s[x][wave] = v[x];
     }
     __syncthreads();
+    for (int w = 0; w < (int)blockDim.x / 64; ++w)
 #pragma unroll
-    for (int x = 0; x < N; ++x) {
-        v[x] = s[x][0];
-        for (int w = 1; w < kCutThreads / 64; ++w) v[x] = join(v[x], s[x][w]);
-    }
+        for (int x = 0; x < N; ++x) v[x] = w == 0 ? s[x][0] : join(v[x], s[x][w]);
     __syncthreads();
 }
 
 // Cuts the call: lengths of the pieces by the rules of the other calls (few_rows_piece, the model of many_rows_piece), and the running sums of the
-// shares' workgroups, from which these find theirs.  Bound by the latency of a few loads that wait for each other.
+// shares' workgroups, from which these find theirs.  As many threads as shares, EACH to a thread where there are more than 1024.  Bound by the latency
+// of a few loads and sums that wait for each other.
+template <int EACH>
 __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, PagedPart few, PagedPart many) {
     __shared__ long long s_sum[8][kCutThreads / 64];
     __shared__ int s_scan[2][2][kCutThreads / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = 2 * a.B;
-    int tiles[kCutEach], keys[kCutEach];           // of share kCutThreads i + tid; tiles of the kernel for many rows negative
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = 2 * a.B, threads = blockDim.x;
+    int tiles[EACH], keys[EACH];           // of share threads * i + tid; tiles of the kernel for many rows negative
     auto add = [](long long x, long long y) { return x + y; };
     auto top = [](long long x, long long y) { return x > y ? x : y; };
     long long sums[3] = {0, 0, 0};                 // (row tile, key tile) pairs of few and many rows, row tiles of many
 #pragma unroll
-    for (int i = 0; i < kCutEach; ++i) {
+    for (int i = 0; i < EACH; ++i) {
         tiles[i] = keys[i] = 0;
-        const int e = kCutThreads * i + tid;
-        if (kCutThreads * i >= E) continue;
+        const int e = threads * i + tid;
+        if (threads * i >= E) continue;
         int kv;
         const SharedRange r = shared_range(a, e, kv);
         if (e >= E) continue;
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, Pag
 
     // many rows: the least time of four lengths
     const int least = shortest_piece(work, many);
-    auto pieces_of = [&](long long n) { return n > row_tiles ? piece_within((work + n - row_tiles - 1) / (n - row_tiles), many) : kWholeAxis; };
+    auto pieces_of = [&](long long n) { return n > row_tiles ? piece_within((long long)ceilf((float)work / (float)(n - row_tiles)), many) : kWholeAxis; };
     const int fit = pieces_of(512);
     int p[4] = {kWholeAxis, fit, fit < 8 ? 4 * fit : pieces_of(1024), fit < kWholeAxis / 2 ? 2 * fit : kWholeAxis};
     long long units[4] = {0, 0, 0, 0}, longest[4] = {0, 0, 0, 0};
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, Pag
     for (int t = 0; t < 4; ++t) {
         p[t] = p[t] < least ? least : (p[t] > kWholeAxis ? kWholeAxis : p[t]);
 #pragma unroll
-        for (int i = 0; i < kCutEach; ++i) {
+        for (int i = 0; i < EACH; ++i) {
             if (tiles[i] >= 0) continue;
             const int splits = keys[i] <= p[t] ? 1 : (keys[i] + p[t] - 1) / p[t];
             units[t] += (long long)-tiles[i] * splits * a.Hkv;
@@ -96,10 +96,10 @@ __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, Pag
     }
 
     int base[2] = {0, 0};
-    for (int i = 0; i < kCutEach && kCutThreads * i < E; ++i) {
+    for (int i = 0; i < EACH && threads * i < E; ++i) {
         int mine_tiles = 0, mine_keys = 0;
 #pragma unroll
-        for (int y = 0; y < kCutEach; ++y) {
+        for (int y = 0; y < EACH; ++y) {
             mine_tiles = y == i ? tiles[y] : mine_tiles;
             mine_keys = y == i ? keys[y] : mine_keys;
         }
@@ -119,10 +119,10 @@ __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, Pag
             if (lane == 63) s_scan[i & 1][x][wave] = v;
         }
         __syncthreads();
-        const int e = kCutThreads * i + tid;
+        const int e = threads * i + tid;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            for (int w = 0; w < kCutThreads / 64; ++w) {
+            for (int w = 0; w < threads / 64; ++w) {
                 if (w == wave) end[x] = min(end[x] + base[x], (int)kMostUnits);
                 base[x] = min(base[x] + s_scan[i & 1][x][w], (int)kMostUnits);
             }
@@ -243,7 +243,9 @@ hipError_t launch_paged_attn_shared(const PagedDims& d, const PagedParts& parts,
                                     const int32_t* shares, const float* slopes_or_null, void* out, float* lse_or_null, hipStream_t st) {
     if ((int64_t)parts.few.n_slots + parts.many.n_slots > 0x7fffffffll) return hipErrorInvalidValue;
     const PagedArgs a = paged_args(d, q, k_pages, vt_pages, exps, block_table, q_starts, kv_lens, shares, slopes_or_null, out, lse_or_null);
-    hipLaunchKernelGGL(paged_cut_kernel, dim3(1), dim3(kCutThreads), 0, st, a, parts.few, parts.many);
+    const int shares_of_call = 2 * d.B, threads = shares_of_call < kCutThreads ? (shares_of_call + 63) / 64 * 64 : kCutThreads;
+    if (shares_of_call <= kCutThreads) hipLaunchKernelGGL(paged_cut_kernel<1>, dim3(1), dim3(threads), 0, st, a, parts.few, parts.many);
+    else hipLaunchKernelGGL(paged_cut_kernel<2 * kMaxRequests / kCutThreads>, dim3(1), dim3(threads), 0, st, a, parts.few, parts.many);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (exps.k != nullptr) e = launch_paged_shared_q8(d, parts, q, k_pages, vt_pages, exps, block_table, q_starts, kv_lens, shares, slopes_or_null, out, lse_or_null, st);
