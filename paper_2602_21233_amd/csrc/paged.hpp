@@ -35,6 +35,14 @@ struct PagedPart {
     int32_t* piece;                   // many rows: key tiles of a piece, as the attention kernel leaves them for the merge
     int32_t* unit_end;                // shared prompts: workgroups up to and with each of the call's 2 B shares
 };
+// What the workgroups of a share need of it, as the kernel that cuts a call leaves it: 32 bytes in one place, loaded at once.
+struct alignas(16) SharedInfo {
+    int32_t first, len;               // rows of q: tokens of the group, or of the request
+    int32_t tile, end;                // key tiles tile .. end - 1
+    int32_t kv;                       // cached tokens of the request
+    int32_t members;                  // of the group whose common part it is; 0: the rest of a request
+    int32_t before, splits;           // first workgroup, and pieces of the key axis
+};
 
 // A request's share of a part: row tiles, key tiles (of its longest row tile), pieces of the key axis
 struct PagedShare {
@@ -114,25 +122,21 @@ __host__ __device__ __forceinline__ PagedShare paged_share(const PagedPart& part
 }
 
 // Shared prompts: share e < B is what group e (the one that starts at request e) has in common, share B + b the rest of request b.
-struct SharedRange {
-    int first, len;                   // rows of q: tokens of the group, or of the request
-    int tile, end;                    // key tiles tile .. end - 1
-    int b;                            // the request whose row of the table names the pages
-};
-// keys: cached tokens of the request (of no group: all that the group has in common); longest axis of any of its row tiles
-__host__ __device__ __forceinline__ PagedShare shared_share(const PagedPart& part, int G, const SharedRange& r, bool common, int kv_len, int sink, int window, int piece) {
-    PagedShare s{0, 0, 0};
+__host__ __device__ __forceinline__ PagedShare shared_share(const PagedPart& part, int G, const SharedInfo& r, int sink, int window) {
+    PagedShare s{0, 0, 1};
     const int64_t rows = (int64_t)r.len * G;
     if (rows > part.row_lo && rows <= part.row_hi) {
-        const int all = (common ? r.end : (kv_len + kPagedTile - 1) / kPagedTile) - r.tile;
+        const bool common = r.members > 0;
+        const int all = (common ? r.end : (r.kv + kPagedTile - 1) / kPagedTile) - r.tile;
         s.tiles = (int)((rows + part.m - 1) >> part.log_m);
-        s.keys = common ? all : most_key_tiles(r.len, kv_len, part.span, sink, window);
+        // the rows of a group are those of several requests, with windows of their own
+        s.keys = common ? all : most_key_tiles(r.len, r.kv, part.span, sink, window);
         if (s.keys > all) s.keys = all;
         if (s.keys < 0) s.keys = 0;
-        s.splits = s.keys <= piece ? 1 : (int)(((uint32_t)s.keys + (uint32_t)piece - 1u) / (uint32_t)piece);
     }
     return s;
 }
+__host__ __device__ __forceinline__ int pieces_for(int keys, int piece) { return keys <= piece ? 1 : (int)(((uint32_t)keys + (uint32_t)piece - 1u) / (uint32_t)piece); }
 
 hipError_t launch_paged_plan(const PagedDims& d, const int32_t* ctx_lens, const int32_t* new_lens, const int32_t* free_pages, int n_free,
                              const int32_t* free_range, int32_t* block_table, int32_t* q_starts, int32_t* kv_lens, int32_t* slots,
@@ -144,6 +148,7 @@ hipError_t launch_paged_append(const PagedDims& d, const void* k, int64_t k_t, i
 // their scratch in bytes.  o and lse are set from ws, which may be null.
 struct PagedParts {
     PagedPart few, many;
+    SharedInfo* infos;                // shared prompts
     size_t ws_bytes;
 };
 PagedParts paged_parts(const PagedDims& d, void* ws_or_null);

@@ -40,6 +40,7 @@ struct PagedArgs {
     int64_t table_stride, q_t, q_h, o_t, o_h, kp_p, kp_h, vp_p, vp_h;
     PagedExps exps;                                   // of a quantised cache
     const int32_t* shares;                            // shared prompts: [3][B]
+    SharedInfo* infos;                                // [2 B]
 };
 // a page value: bf16, or e4m3 (Q8)
 template <bool Q8>
@@ -198,18 +199,19 @@ __device__ __forceinline__ Group group_of(const PagedArgs& a, int b) {
     g.tiles = g.n > 1 && b < g.leader + g.n ? (tokens >> a.log_p << a.log_p) / kPagedTile : 0;
     return g;
 }
-__device__ __forceinline__ SharedRange shared_range(const PagedArgs& a, int e, int& kv) {
-    SharedRange r{0, 0, 0, 0, 0};
-    kv = 0;
+__device__ __forceinline__ SharedInfo shared_range(const PagedArgs& a, int e) {
+    SharedInfo r{0, 0, 0, 0, 0, 0, 0, 0};
     if (e >= 2 * a.B) return r;
-    r.b = e < a.B ? e : e - a.B;
-    const Group g = group_of(a, r.b);
-    const int n = e >= a.B ? 1 : g.leader == r.b && g.tiles > 0 ? g.n : 0;
-    r.first = clamp_int(a.q_starts[r.b], 0, a.T);
-    r.len = clamp_int(a.q_starts[r.b + n], r.first, a.T) - r.first;
-    kv = clamp_int(a.kv_lens[r.b], 0, a.C << a.log_p);
-    r.tile = e < a.B ? 0 : g.tiles;
-    r.end = e < a.B ? g.tiles : kWholeAxis;
+    const int b = e < a.B ? e : e - a.B;
+    const Group g = group_of(a, b);
+    const bool common = e < a.B;
+    const int n = !common ? 1 : g.leader == b && g.tiles > 0 ? g.n : 0;
+    r.first = clamp_int(a.q_starts[b], 0, a.T);
+    r.len = clamp_int(a.q_starts[b + n], r.first, a.T) - r.first;
+    r.tile = common ? 0 : g.tiles;
+    r.end = common ? g.tiles : kWholeAxis;
+    r.kv = clamp_int(a.kv_lens[b], 0, a.C << a.log_p);
+    r.members = common ? n : 0;
     return r;
 }
 // the first of n ascending values that is above v, the same v in every lane; n if there is none
@@ -228,12 +230,12 @@ __device__ __forceinline__ int first_above(const int32_t* values, int n, int v) 
     }
     return n;
 }
-// position of the group's row `token`, found among its requests: where they bring as many tokens each, at the first try
-__device__ __forceinline__ int shared_position(const PagedArgs& a, const SharedRange& r, int members, int token) {
+// position of row `token` of the group that starts at request b0, found among its requests: where they bring as many tokens each, at the first try
+__device__ __forceinline__ int shared_position(const PagedArgs& a, const SharedInfo& r, int b0, int token) {
     const int t = r.first + token;
-    int b = r.b + (int)((int64_t)token * members / r.len);
+    int b = b0 + (int)((int64_t)token * r.members / r.len);
     if (a.q_starts[b] > t || a.q_starts[b + 1] <= t) {
-        int lo = r.b, hi = r.b + members;
+        int lo = b0, hi = b0 + r.members;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (a.q_starts[mid] <= t) lo = mid;
@@ -246,8 +248,7 @@ __device__ __forceinline__ int shared_position(const PagedArgs& a, const SharedR
 // What workgroup `item` of a part serves
 struct SharedUnit {
     Share sh;
-    SharedRange range;
-    int members;                      // of the group whose common part it is; 0: the rest of a request
+    SharedInfo range;
     bool partial;
 };
 __device__ __forceinline__ SharedUnit shared_unit(const PagedArgs& a, const PagedPart& part, int item) {
@@ -255,17 +256,15 @@ __device__ __forceinline__ SharedUnit shared_unit(const PagedArgs& a, const Page
     const int e = first_above(part.unit_end, 2 * a.B, item);
     u.sh.b = -1;
     if (e >= 2 * a.B) return u;
-    int kv;
-    u.range = shared_range(a, e, kv);
-    u.members = e < a.B ? group_of(a, u.range.b).n : 0;
-    u.sh.s = shared_share(part, a.G, u.range, e < a.B, kv, a.sink, a.window, *part.piece);
+    u.range = a.infos[e];
+    u.sh.s = shared_share(part, a.G, u.range, a.sink, a.window);
     if (u.sh.s.tiles == 0) return u;
-    u.sh.b = u.range.b;
-    const int before = e > 0 ? part.unit_end[e - 1] : 0;
-    u.sh.unit = item - before;
-    u.sh.slot = before;
-    u.sh.r = Request{u.range.first, u.range.len, kv};
-    u.partial = u.range.tile > 0 || e < a.B || u.sh.s.splits > 1;
+    u.sh.s.splits = u.range.splits;
+    u.sh.b = e < a.B ? e : e - a.B;
+    u.sh.unit = item - u.range.before;
+    u.sh.slot = u.range.before;
+    u.sh.r = Request{u.range.first, u.range.len, u.range.kv};
+    u.partial = u.range.tile > 0 || u.range.members > 0 || u.range.splits > 1;
     return u;
 }
 
@@ -399,11 +398,11 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
 #pragma unroll
     for (int f = 0; f < MF; ++f) pos[f] = pos0 + min(row0 + 16 * f + n16, last_row) / a.G;
     if constexpr (SHARED) {
-        if (unit.members > 0) {                                 // rows of several requests
+        if (unit.range.members > 0) {                                 // rows of several requests
             int lo = 0x7fffffff, hi = -0x7fffffff;
 #pragma unroll
             for (int f = 0; f < MF; ++f) {
-                pos[f] = shared_position(a, unit.range, unit.members, min(row0 + 16 * f + n16, last_row) / a.G);
+                pos[f] = shared_position(a, unit.range, sh.b, min(row0 + 16 * f + n16, last_row) / a.G);
                 lo = min(lo, pos[f]);
                 hi = max(hi, pos[f]);
             }
@@ -958,9 +957,9 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     const int wave_row = row0 + 32 * wave;                                    // wave-uniform bounds of this wavefront's rows
     int wave_lo = pos0 + min(wave_row, last_row) / a.G, wave_hi = pos0 + min(wave_row + 31, last_row) / a.G;
     if constexpr (SHARED) {
-        if (unit.members > 0) {                                               // rows of several requests: a lane finds two of the 128
-            const int p0 = shared_position(a, unit.range, unit.members, min(row0 + lane, last_row) / a.G);
-            const int p1 = shared_position(a, unit.range, unit.members, min(row0 + 64 + lane, last_row) / a.G);
+        if (unit.range.members > 0) {                                               // rows of several requests: a lane finds two of the 128
+            const int p0 = shared_position(a, unit.range, sh.b, min(row0 + lane, last_row) / a.G);
+            const int p1 = shared_position(a, unit.range, sh.b, min(row0 + 64 + lane, last_row) / a.G);
             const int from = 32 * (wave & 1) + l32, q0 = __shfl(p0, from), q1 = __shfl(p1, from);
             pos = wave < 2 ? q0 : q1;
             int lo = pos, hi = pos, lo_all = min(p0, p1), hi_all = max(p0, p1);
@@ -1676,11 +1675,11 @@ hipError_t launch_shared_parts(const PagedArgs& a, const PagedParts& parts, hipS
 }
 
 PagedArgs paged_args(const PagedDims& d, const void* q, const void* k_pages, const void* vt_pages, const PagedExps& exps, const int32_t* block_table,
-                     const int32_t* q_starts, const int32_t* kv_lens, const int32_t* shares_or_null, const float* slopes_or_null, void* out,
-                     float* lse_or_null) {
+                     const int32_t* q_starts, const int32_t* kv_lens, const int32_t* shares_or_null, SharedInfo* infos_or_null, const float* slopes_or_null,
+                     void* out, float* lse_or_null) {
     return {(const uint16_t*)q, k_pages, vt_pages, block_table, q_starts, kv_lens, slopes_or_null,
             (uint16_t*)out, lse_or_null, d.B, d.Hq, d.Hkv, d.G, d.T, d.log_p, d.n_pages, d.C, d.sink, d.window, d.scale, d.cap,
-            d.table_stride, d.q_t, d.q_h, d.o_t, d.o_h, d.kp_p, d.kp_h, d.vp_p, d.vp_h, exps, shares_or_null};
+            d.table_stride, d.q_t, d.q_h, d.o_t, d.o_h, d.kp_p, d.kp_h, d.vp_p, d.vp_h, exps, shares_or_null, infos_or_null};
 }
 
 }  // namespace

@@ -36,20 +36,16 @@ __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, Pag
     __shared__ long long s_sum[8][kCutThreads / 64];
     __shared__ int s_scan[2][2][kCutThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = 2 * a.B, threads = blockDim.x;
-    int tiles[EACH], keys[EACH];           // of share threads * i + tid; tiles of the kernel for many rows negative
+    SharedInfo info[EACH];                         // of share threads * i + tid
+    int tiles[EACH], keys[EACH];                   // tiles of the kernel for many rows negative
     auto add = [](long long x, long long y) { return x + y; };
     auto top = [](long long x, long long y) { return x > y ? x : y; };
     long long sums[3] = {0, 0, 0};                 // (row tile, key tile) pairs of few and many rows, row tiles of many
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        tiles[i] = keys[i] = 0;
-        const int e = threads * i + tid;
-        if (threads * i >= E) continue;
-        int kv;
-        const SharedRange r = shared_range(a, e, kv);
-        if (e >= E) continue;
-        const PagedShare f = few.m ? shared_share(few, a.G, r, e < a.B, kv, a.sink, a.window, kWholeAxis) : PagedShare{0, 0, 0};
-        const PagedShare m = shared_share(many, a.G, r, e < a.B, kv, a.sink, a.window, kWholeAxis);
+        info[i] = shared_range(a, threads * i + tid);          // empty behind the last share
+        const PagedShare f = few.m ? shared_share(few, a.G, info[i], a.sink, a.window) : PagedShare{0, 0, 1};
+        const PagedShare m = shared_share(many, a.G, info[i], a.sink, a.window);
         tiles[i] = f.tiles > 0 ? f.tiles : -m.tiles;
         keys[i] = f.tiles > 0 ? f.keys : m.keys;
         sums[0] += (long long)f.tiles * f.keys;
@@ -72,7 +68,7 @@ __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, Pag
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             if (tiles[i] >= 0) continue;
-            const int splits = keys[i] <= p[t] ? 1 : (keys[i] + p[t] - 1) / p[t];
+            const int splits = pieces_for(keys[i], p[t]);
             units[t] += (long long)-tiles[i] * splits * a.Hkv;
             longest[t] = top(longest[t], keys[i] < p[t] ? keys[i] : p[t]);
         }
@@ -90,26 +86,16 @@ __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, Pag
             many_piece = p[t];
         }
     }
-    if (tid == 0) {
-        *few.piece = few_piece;
-        *many.piece = many_piece;
-    }
-
     int base[2] = {0, 0};
-    for (int i = 0; i < EACH && threads * i < E; ++i) {
-        int mine_tiles = 0, mine_keys = 0;
 #pragma unroll
-        for (int y = 0; y < EACH; ++y) {
-            mine_tiles = y == i ? tiles[y] : mine_tiles;
-            mine_keys = y == i ? keys[y] : mine_keys;
-        }
-        int end[2];
+    for (int i = 0; i < EACH; ++i) {
+        if (threads * i >= E) break;
+        int end[2], own[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const int piece = x ? many_piece : few_piece, n = x ? -mine_tiles : mine_tiles;
-            const int splits = mine_keys <= piece ? 1 : (mine_keys + piece - 1) / piece;
-            const long long own = n > 0 ? (long long)n * splits * a.Hkv : 0;
-            int v = (int)(own < kMostUnits ? own : kMostUnits);
+            const int n = x ? -tiles[i] : tiles[i];
+            const long long units = n > 0 ? (long long)n * pieces_for(keys[i], x ? many_piece : few_piece) * a.Hkv : 0;
+            int v = own[x] = (int)(units < kMostUnits ? units : kMostUnits);
 #pragma unroll
             for (int y = 1; y < 64; y <<= 1) {
                 const int u = __shfl_up(v, y);
@@ -128,6 +114,12 @@ __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, Pag
             }
             if (e < E && (x == 1 || few.m)) (x ? many : few).unit_end[e] = end[x];
         }
+        if (e < E) {
+            const bool is_few = tiles[i] > 0;
+            info[i].before = (is_few ? end[0] : end[1]) - (is_few ? own[0] : own[1]);
+            info[i].splits = tiles[i] == 0 ? 0 : pieces_for(keys[i], is_few ? few_piece : many_piece);
+            a.infos[e] = info[i];
+        }
     }
 }
 
@@ -143,19 +135,13 @@ __global__ __launch_bounds__(256) void paged_shared_merge_kernel(PagedArgs a, Pa
         const int head = (int)(item / NV % a.Hq), t = (int)(item / NV / a.Hq), kvh = head / a.G;
         const int b = first_above(a.q_starts + 1, a.B, t);
         if (b >= a.B || a.q_starts[b] > t) continue;               // padding
-        const Group g = group_of(a, b);
+        const SharedInfo rest = a.infos[a.B + b];
+        const SharedInfo common = a.infos[clamp_int(a.shares[b], 0, b)];
+        if (rest.tile == 0 && rest.splits <= 1) continue;
         PieceSums sums;
-        bool there = g.tiles > 0;
-        int pos = 0;
-#pragma unroll 1
-        for (int x = 0; x < 2; ++x) {                              // the group's part, the request's own
-            if (x == 0 && g.tiles == 0) continue;
-            int kv;
-            const int e = x == 0 ? g.leader : a.B + b;
-            const SharedRange r = shared_range(a, e, kv);
-            if (x == 1) pos = kv - r.len + t - r.first;
+        auto add = [&](const SharedInfo& r) {
             const int64_t rows = (int64_t)r.len * a.G, row = (int64_t)(t - r.first) * a.G + head % a.G;
-            if (row < 0 || row >= rows) continue;
+            if (row < 0 || row >= rows || r.splits < 1) return;
             PagedPart part = many;                                 // by its fields: the struct itself would be chosen in memory
             if (few.m && rows <= few.row_hi) {
                 part.m = few.m;
@@ -163,18 +149,14 @@ __global__ __launch_bounds__(256) void paged_shared_merge_kernel(PagedArgs a, Pa
                 part.n_slots = few.n_slots;
                 part.o = few.o;
                 part.lse = few.lse;
-                part.unit_end = few.unit_end;
             }
-            const int before = e > 0 ? part.unit_end[e - 1] : 0, units = part.unit_end[e] - before;
-            const int tiles = (int)((rows + part.m - 1) >> part.log_m);
-            const int splits = units / a.Hkv / tiles;
-            if (splits > 1) there = true;
-            if (!there) continue;
-            const int64_t slot0 = before + (tiles - 1 - (row >> part.log_m)) * splits * a.Hkv + kvh;
-            if (slot0 < 0 || splits < 1 || slot0 + (int64_t)(splits - 1) * a.Hkv >= part.n_slots) continue;      // malformed: more than there is room for
-            add_pieces<D, NV>(part, (int)slot0, a.Hkv, splits, (int)row & (part.m - 1), d0, sums);
-        }
-        if (there) finish_row<D, NV>(a, sums, t, head, pos, d0);
+            const int64_t tiles = (rows + part.m - 1) >> part.log_m, slot0 = r.before + (tiles - 1 - (row >> part.log_m)) * r.splits * a.Hkv + kvh;
+            if (slot0 < 0 || slot0 + (int64_t)(r.splits - 1) * a.Hkv >= part.n_slots) return;      // malformed: more than there is room for
+            add_pieces<D, NV>(part, (int)slot0, a.Hkv, r.splits, (int)row & (part.m - 1), d0, sums);
+        };
+        if (rest.tile > 0) add(common);
+        add(rest);
+        finish_row<D, NV>(a, sums, t, head, rest.kv - rest.len + t - rest.first, d0);
     }
 }
 
@@ -231,9 +213,9 @@ PagedParts paged_shared_parts(const PagedDims& d, void* ws_or_null) {
             part->unit_end = (int32_t*)(base + off);
             off += ((size_t)2 * d.B * sizeof(int32_t) + 255) / 256 * 256;
         }
-        part->piece = (int32_t*)(base + off);
-        off += 256;
     }
+    p.infos = (SharedInfo*)((char*)ws_or_null + off);
+    off += (size_t)2 * d.B * sizeof(SharedInfo);
     p.ws_bytes = off;
     return p;
 }
@@ -242,7 +224,7 @@ hipError_t launch_paged_attn_shared(const PagedDims& d, const PagedParts& parts,
                                     const PagedExps& exps, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens,
                                     const int32_t* shares, const float* slopes_or_null, void* out, float* lse_or_null, hipStream_t st) {
     if ((int64_t)parts.few.n_slots + parts.many.n_slots > 0x7fffffffll) return hipErrorInvalidValue;
-    const PagedArgs a = paged_args(d, q, k_pages, vt_pages, exps, block_table, q_starts, kv_lens, shares, slopes_or_null, out, lse_or_null);
+    const PagedArgs a = paged_args(d, q, k_pages, vt_pages, exps, block_table, q_starts, kv_lens, shares, parts.infos, slopes_or_null, out, lse_or_null);
     const int shares_of_call = 2 * d.B, threads = shares_of_call < kCutThreads ? (shares_of_call + 63) / 64 * 64 : kCutThreads;
     if (shares_of_call <= kCutThreads) hipLaunchKernelGGL(paged_cut_kernel<1>, dim3(1), dim3(threads), 0, st, a, parts.few, parts.many);
     else hipLaunchKernelGGL(paged_cut_kernel<2 * kMaxRequests / kCutThreads>, dim3(1), dim3(threads), 0, st, a, parts.few, parts.many);
