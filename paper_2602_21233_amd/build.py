@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparse_prefill.so")
 SOURCES = ("api.hip", "pool.hip", "select.hip", "select_d128.hip", "select_d64.hip", "attn.hip",
-           "paged_api.hip", "paged_cache.hip", "paged_attn.hip", "paged_attn_q8.hip", "paged_attn_shared.hip", "paged_attn_shared_q8.hip", "paged_q8.hip", "paged_shares.hip")
+           "paged_api.hip", "paged_cache.hip", "paged_attn.hip", "paged_attn_q8.hip", "paged_attn_shared.hip", "paged_attn_shared_q8.hip", "paged_q8.hip", "paged_shared.hip", "paged_shares.hip")
 HEADERS = ("attn_parts.hpp", "common.hpp", "e4m3.hpp", "overlap.hpp", "paged.hpp", "paged_attn_impl.hpp", "row_deal.hpp", "score_rows.hpp", "select_impl.hpp", "value_block.hpp", os.path.join("..", "..", "include", "sparse_prefill.h"))
 
 # The attention kernel never produces NaN from finite inputs; telling the compiler so

@@ -172,6 +172,9 @@ PagedParts paged_shared_parts(const PagedDims& d, void* ws_or_null);
 hipError_t launch_paged_shared_q8(const PagedDims& d, const PagedParts& parts, const void* q, const void* k_pages, const void* vt_pages,
                                   const PagedExps& exps, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens,
                                   const int32_t* shares, const float* slopes_or_null, void* out, float* lse_or_null, hipStream_t st);
+hipError_t launch_paged_shared_bf16(const PagedDims& d, const PagedParts& parts, const void* q, const void* k_pages, const void* vt_pages,
+                                    const PagedExps& exps, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens,
+                                    const int32_t* shares, const float* slopes_or_null, void* out, float* lse_or_null, hipStream_t st);
 hipError_t launch_paged_attn_shared(const PagedDims& d, const PagedParts& parts, const void* q, const void* k_pages, const void* vt_pages,
                                     const PagedExps& exps, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens,
                                     const int32_t* shares, const float* slopes_or_null, void* out, float* lse_or_null, hipStream_t st);

@@ -1,0 +1,245 @@
+// Attention of requests that share prompts: how a call is cut, and the merge.
+//
+// What a group of requests has in common is one range of keys for the rows of all of them, and every request has the rest of its own (paged.hpp:
+// shares).  Three launches: one workgroup cuts the call, the attention kernels of the other paged calls go through the ranges and leave partial
+// results, and a wavefront for each row joins those of its group's part and of its own.
+#include "paged_attn_impl.hpp"
+
+namespace spa {
+namespace {
+
+constexpr int kCutThreads = 1024;
+constexpr int64_t kMostUnits = 1 << 30;
+
+// sum or maximum over the workgroup, in every thread
+template <int N, typename T, typename F>
+__device__ __forceinline__ void over_workgroup(T (&v)[N], T (*s)[kCutThreads / 64], F&& join) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+#pragma unroll
+        for (int y = 1; y < 64; y <<= 1) v[x] = join(v[x], (T)__shfl_xor(v[x], y));
+        if (lane == 0) s[x][wave] = v[x];
+    }
+    __syncthreads();
+    for (int w = 0; w < (int)blockDim.x / 64; ++w)
+#pragma unroll
+        for (int x = 0; x < N; ++x) v[x] = w == 0 ? s[x][0] : join(v[x], s[x][w]);
+    __syncthreads();
+}
+
+// Cuts the call: lengths of the pieces by the rules of the other calls (few_rows_piece, the model of many_rows_piece), and the running sums of the
+// shares' workgroups, from which these find theirs.  As many threads as shares, EACH to a thread where there are more than 1024.  Bound by the latency
+// of a few loads and sums that wait for each other.
+template <int EACH>
+__global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, PagedPart few, PagedPart many) {
+    __shared__ long long s_sum[8][kCutThreads / 64];
+    __shared__ int s_scan[2][2][kCutThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = 2 * a.B, threads = blockDim.x;
+    SharedInfo info[EACH];                         // of share threads * i + tid
+    int tiles[EACH], keys[EACH];                   // tiles of the kernel for many rows negative
+    auto add = [](long long x, long long y) { return x + y; };
+    auto top = [](long long x, long long y) { return x > y ? x : y; };
+    long long sums[3] = {0, 0, 0};                 // (row tile, key tile) pairs of few and many rows, row tiles of many
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        info[i] = shared_range(a, threads * i + tid);          // empty behind the last share
+        const PagedShare f = few.m ? shared_share(few, a.G, info[i], a.sink, a.window) : PagedShare{0, 0, 1};
+        const PagedShare m = shared_share(many, a.G, info[i], a.sink, a.window);
+        tiles[i] = f.tiles > 0 ? f.tiles : -m.tiles;
+        keys[i] = f.tiles > 0 ? f.keys : m.keys;
+        sums[0] += (long long)f.tiles * f.keys;
+        sums[1] += (long long)m.tiles * m.keys;
+        sums[2] += m.tiles;
+    }
+    over_workgroup(sums, s_sum, add);
+    const long long work = sums[1] * a.Hkv, row_tiles = sums[2] * a.Hkv;
+    const int few_piece = few.m ? few_rows_piece(sums[0] * a.Hkv, few) : kWholeAxis;
+
+    // many rows: the least time of four lengths
+    const int least = shortest_piece(work, many);
+    auto pieces_of = [&](long long n) { return n > row_tiles ? piece_within((long long)ceilf((float)work / (float)(n - row_tiles)), many) : kWholeAxis; };
+        // 512 workgroups run at once.  Those of few rows go beside the others, which get their share of the places by time: a key tile of few rows is
+    // bound by the memory and counts for one and a half of many rows', but 200 of them have all that the memory gives (16 requests
+    // of 7 prompts of 23000, as much of either: 212 us with 178 places for many rows, 176 with 512).  64 requests of 4 prompts, 8000 key tiles of many rows and 6144 of few, with 256, 384,
+    // 512 and 1024 pieces of many rows: 110.8, 115.5, 119.5 and 131.6 us; 8 behind 100000, 12500 and 448: 119.5, 113.6, 102.7 and 120.0.
+    const float share = sums[1] > 0 ? (float)sums[1] / ((float)sums[1] + 1.5f * (float)sums[0]) : 1.f;
+    const int places = max(312, (int)(512.f * share));
+    const int fit = pieces_of(places);
+    int p[4] = {kWholeAxis, fit, fit < kWholeAxis / 4 ? 2 * fit : kWholeAxis, fit < kWholeAxis / 4 ? 4 * fit : kWholeAxis};
+    long long units[4] = {0, 0, 0, 0}, longest[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        p[t] = p[t] < least ? least : (p[t] > kWholeAxis ? kWholeAxis : p[t]);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (tiles[i] >= 0) continue;
+            const int splits = pieces_for(keys[i], p[t]);
+            units[t] += (long long)-tiles[i] * splits * a.Hkv;
+            longest[t] = top(longest[t], keys[i] < p[t] ? keys[i] : p[t]);
+        }
+    }
+    over_workgroup(units, s_sum, add);
+    over_workgroup(longest, s_sum, top);
+    int many_piece = p[0];
+    float best = INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const float n = (float)(units[t] > 1 ? units[t] : 1);
+        const float us = 1.6f * fmaxf((float)longest[t], ceilf(n / (float)places) * (float)work / n) + 0.03f * n;
+        if (us < best) {
+            best = us;
+            many_piece = p[t];
+        }
+    }
+    int base[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (threads * i >= E) break;
+        int end[2], own[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int n = x ? -tiles[i] : tiles[i];
+            const long long units = n > 0 ? (long long)n * pieces_for(keys[i], x ? many_piece : few_piece) * a.Hkv : 0;
+            int v = own[x] = (int)(units < kMostUnits ? units : kMostUnits);
+#pragma unroll
+            for (int y = 1; y < 64; y <<= 1) {
+                const int u = __shfl_up(v, y);
+                if (lane >= y) v = min(v + u, (int)kMostUnits);
+            }
+            end[x] = v;
+            if (lane == 63) s_scan[i & 1][x][wave] = v;
+        }
+        __syncthreads();
+        const int e = threads * i + tid;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            for (int w = 0; w < threads / 64; ++w) {
+                if (w == wave) end[x] = min(end[x] + base[x], (int)kMostUnits);
+                base[x] = min(base[x] + s_scan[i & 1][x][w], (int)kMostUnits);
+            }
+            if (e < E && (x == 1 || few.m)) (x ? many : few).unit_end[e] = end[x];
+        }
+        if (e < E) {
+            const bool is_few = tiles[i] > 0;
+            info[i].before = (is_few ? end[0] : end[1]) - (is_few ? own[0] : own[1]);
+            info[i].splits = tiles[i] == 0 ? 0 : pieces_for(keys[i], is_few ? few_piece : many_piece);
+            a.infos[e] = info[i];
+        }
+    }
+}
+
+// A wavefront joins the results of a row's (or of a quarter of its dims') two parts.  Where a request shares nothing and has not been cut, its row is there
+// already.
+template <int D, int NV>
+__global__ __launch_bounds__(256) void paged_shared_merge_kernel(PagedArgs a, PagedPart few, PagedPart many) {
+    constexpr int DV = D / NV, LPR = DV / 4;
+    const int lane = threadIdx.x & 63;
+    const int64_t items = (int64_t)a.T * a.Hq * NV;
+    for (int64_t item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += gridDim.x * 4) {
+        const int d0 = (int)(item % NV) * DV + 4 * (lane % LPR);
+        const int head = (int)(item / NV % a.Hq), t = (int)(item / NV / a.Hq), kvh = head / a.G;
+        const int b = first_above(a.q_starts + 1, a.B, t);
+        if (b >= a.B || a.q_starts[b] > t) continue;               // padding
+        const SharedInfo rest = a.infos[a.B + b];
+        const SharedInfo common = a.infos[clamp_int(a.shares[b], 0, b)];
+        if (rest.tile == 0 && rest.splits <= 1) continue;
+        PieceSums sums;
+        auto add = [&](const SharedInfo& r) {
+            const int64_t rows = (int64_t)r.len * a.G, row = (int64_t)(t - r.first) * a.G + head % a.G;
+            if (row < 0 || row >= rows || r.splits < 1) return;
+            PagedPart part = many;                                 // by its fields: the struct itself would be chosen in memory
+            if (few.m && rows <= few.row_hi) {
+                part.m = few.m;
+                part.log_m = few.log_m;
+                part.n_slots = few.n_slots;
+                part.o = few.o;
+                part.lse = few.lse;
+            }
+            const int64_t tiles = (rows + part.m - 1) >> part.log_m, slot0 = r.before + (tiles - 1 - (row >> part.log_m)) * r.splits * a.Hkv + kvh;
+            if (slot0 < 0 || slot0 + (int64_t)(r.splits - 1) * a.Hkv >= part.n_slots) return;      // malformed: more than there is room for
+            add_pieces<D, NV>(part, (int)slot0, a.Hkv, r.splits, (int)row & (part.m - 1), d0, sums);
+        };
+        if (rest.tile > 0) add(common);
+        add(rest);
+        finish_row<D, NV>(a, sums, t, head, rest.kv - rest.len + t - rest.first, d0);
+    }
+}
+
+// Most workgroups of a part, each of which has room for its partial result: `shares` ranges of `rows` rows in all, 2^log_most more for cuts.
+int64_t most_shared_units(const PagedDims& d, const PagedPart& part, int64_t shares, int64_t rows) {
+    const int64_t tiles = (rows / part.m + shares) * d.Hkv;
+    const int64_t most = 1ll << part.log_most, cuts = ((((int64_t)d.C << d.log_p) + kPagedTile - 1) / kPagedTile + part.min_tiles - 1) / part.min_tiles;
+    return tiles * cuts < tiles + most ? tiles * cuts : tiles + most;
+}
+
+template <int D>
+hipError_t launch_merge(const PagedArgs& a, const PagedParts& parts, hipStream_t st) {
+    const int64_t rows = (int64_t)a.T * a.Hq;
+    if (rows <= 1024) hipLaunchKernelGGL((paged_shared_merge_kernel<D, 4>), dim3((unsigned)rows), dim3(256), 0, st, a, parts.few, parts.many);
+    else hipLaunchKernelGGL((paged_shared_merge_kernel<D, 1>), dim3((unsigned)(rows < 8192 ? (rows + 3) / 4 : 2048)), dim3(256), 0, st, a, parts.few, parts.many);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+PagedParts paged_shared_parts(const PagedDims& d, void* ws_or_null) {
+    PagedParts p{};
+    const int few_rows = d.G <= 16 ? 16 : 32;
+    const int64_t requests = d.B < d.T ? d.B : d.T, groups = d.B / 2 < requests ? d.B / 2 : requests;        // with rows
+    const int64_t rows = 2 * (int64_t)d.T * d.G;     // a token is in one request's rest, and in one group's common part
+    if (d.G <= few_rows) {
+        p.few.m = few_rows;
+        p.few.log_m = few_rows == 16 ? 4 : 5;
+        p.few.log_most = 11;
+        p.few.min_tiles = 4;
+        p.few.row_hi = few_rows;
+        p.few.n_slots = 1;
+    }
+    p.many.m = kManyRows;
+    p.many.log_m = 7;
+    p.many.log_most = 10;
+    p.many.min_tiles = 2;
+    p.many.row_lo = p.few.m ? few_rows : 0;
+    p.many.row_hi = 0x7fffffff;
+    const int64_t long_ones = rows / (p.many.row_lo + 1);         // at most so many have more than few rows
+    size_t off = 0;
+    for (PagedPart* part : {&p.few, &p.many}) {
+        char* base = (char*)ws_or_null;
+        part->span = (part->m + d.G - 1) / d.G + 1;
+        const bool is_few = part == &p.few;
+        if (part->m > 0) {
+            const int64_t shares = is_few || long_ones > requests + groups ? requests + groups : long_ones;
+            const int64_t units = most_shared_units(d, *part, shares, is_few ? 0 : rows);
+            part->n_slots = (int)(units < kMostUnits ? units : kMostUnits);
+            part->o = (float*)(base + off);
+            off += (size_t)part->n_slots * part->m * d.D * sizeof(float);
+            part->lse = (float*)(base + off);
+            off += ((size_t)part->n_slots * part->m * sizeof(float) + 255) / 256 * 256;
+            part->unit_end = (int32_t*)(base + off);
+            off += ((size_t)2 * d.B * sizeof(int32_t) + 255) / 256 * 256;
+        }
+    }
+    p.infos = (SharedInfo*)((char*)ws_or_null + off);
+    off += (size_t)2 * d.B * sizeof(SharedInfo);
+    p.ws_bytes = off;
+    return p;
+}
+
+hipError_t launch_paged_attn_shared(const PagedDims& d, const PagedParts& parts, const void* q, const void* k_pages, const void* vt_pages,
+                                    const PagedExps& exps, const int32_t* block_table, const int32_t* q_starts, const int32_t* kv_lens,
+                                    const int32_t* shares, const float* slopes_or_null, void* out, float* lse_or_null, hipStream_t st) {
+    if ((int64_t)parts.few.n_slots + parts.many.n_slots > 0x7fffffffll) return hipErrorInvalidValue;
+    const PagedArgs a = paged_args(d, q, k_pages, vt_pages, exps, block_table, q_starts, kv_lens, shares, parts.infos, slopes_or_null, out, lse_or_null);
+    const int shares_of_call = 2 * d.B, threads = shares_of_call < kCutThreads ? (shares_of_call + 63) / 64 * 64 : kCutThreads;
+    if (shares_of_call <= kCutThreads) hipLaunchKernelGGL(paged_cut_kernel<1>, dim3(1), dim3(threads), 0, st, a, parts.few, parts.many);
+    else hipLaunchKernelGGL(paged_cut_kernel<2 * kMaxRequests / kCutThreads>, dim3(1), dim3(threads), 0, st, a, parts.few, parts.many);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const auto attend = exps.k != nullptr ? launch_paged_shared_q8 : launch_paged_shared_bf16;
+    e = attend(d, parts, q, k_pages, vt_pages, exps, block_table, q_starts, kv_lens, shares, slopes_or_null, out, lse_or_null, st);
+    if (e != hipSuccess) return e;
+    return d.D == 128 ? launch_merge<128>(a, parts, st) : launch_merge<64>(a, parts, st);
+}
+
+}  // namespace spa
