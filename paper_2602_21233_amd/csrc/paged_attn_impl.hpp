@@ -568,7 +568,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
                 w[r / 8][r % 8] = __builtin_amdgcn_exp2f(x[r / 8][r % 8] - mr);
                 sum += w[r / 8][r % 8];
             }
-            if (__any(m[f] == -INFINITY || !(l[f] + sum < kRescaleAt))) {
+            if (__any(m[f] == -INFINITY || l[f] + sum >= kRescaleAt)) {     // a NaN row stays as it is, and others keep their references
                 float mx = x[0][0];
 #pragma unroll
                 for (int r = 1; r < NX; ++r) mx = fmaxf(mx, x[r / 8][r % 8]);
@@ -1357,7 +1357,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         };
         SPA_FENCE();
         static_for<NG>([&](auto g_tag) { group(g_tag); });
-        if (needs_mask(key0) || __any(!(l_new < kRescaleAt))) slow_weights(s_cur, key0, pn0, pn1);
+        if (needs_mask(key0) || __any(l_new >= kRescaleAt)) slow_weights(s_cur, key0, pn0, pn1);
         else l = l_new;
     };
 

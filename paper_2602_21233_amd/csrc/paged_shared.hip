@@ -61,10 +61,10 @@ __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, Pag
     auto pieces_of = [&](long long n) { return n > row_tiles ? piece_within((long long)ceilf((float)work / (float)(n - row_tiles)), many) : kWholeAxis; };
         // 512 workgroups run at once.  Those of few rows go beside the others, which get their share of the places by time: a key tile of few rows is
     // bound by the memory and counts for one and a half of many rows', but 200 of them have all that the memory gives (16 requests
-    // of 7 prompts of 23000, as much of either: 212 us with 178 places for many rows, 176 with 512).  64 requests of 4 prompts, 8000 key tiles of many rows and 6144 of few, with 256, 384,
+    // of 7 prompts of 23000, as much of either: 212 us with 178 places for many rows, 157 with 280, 176 with 512).  64 requests of 4 prompts, 8000 key tiles of many rows and 6144 of few, with 256, 384,
     // 512 and 1024 pieces of many rows: 110.8, 115.5, 119.5 and 131.6 us; 8 behind 100000, 12500 and 448: 119.5, 113.6, 102.7 and 120.0.
     const float share = sums[1] > 0 ? (float)sums[1] / ((float)sums[1] + 1.5f * (float)sums[0]) : 1.f;
-    const int places = max(312, (int)(512.f * share));
+    const int places = max(280, (int)(512.f * share));
     const int fit = pieces_of(places);
     int p[4] = {kWholeAxis, fit, fit < kWholeAxis / 4 ? 2 * fit : kWholeAxis, fit < kWholeAxis / 4 ? 4 * fit : kWholeAxis};
     long long units[4] = {0, 0, 0, 0}, longest[4] = {0, 0, 0, 0};
