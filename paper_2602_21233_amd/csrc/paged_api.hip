@@ -220,7 +220,7 @@ int sparse_prefill_paged_read(const spa_paged_params* p, const void* k_pages, co
     const Rows read[] = {page_rows(p, k_pages, p->kp_stride, bytes), page_rows(p, vt_pages, p->vp_stride, bytes), k_exp_rows(p, exps_or_null),
                          v_exp_rows(p, exps_or_null), table_rows(p, block_table), words_of(starts, p->batch + 1), words_of(kv_lens, p->batch)};
     const Rows written[] = {token_rows(p, k, p->k_stride, p->n_kv_heads), token_rows(p, v, p->v_stride, p->n_kv_heads)};
-    if (clash(written, read)) return SPA_ERR_OVERLAP;
+    if (clash(written, read) || k_pages == vt_pages || (exps_or_null && exps_or_null->k == exps_or_null->v)) return SPA_ERR_OVERLAP;
     return launch_code(launch_paged_read(paged_dims(p), k_pages, vt_pages, paged_exps(exps_or_null), block_table, starts, kv_lens, k, p->k_stride[0],
                                          p->k_stride[1], v, p->v_stride[0], p->v_stride[1], (hipStream_t)hip_stream));
 }

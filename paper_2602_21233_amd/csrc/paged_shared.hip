@@ -221,7 +221,7 @@ PagedParts paged_shared_parts(const PagedDims& d, void* ws_or_null) {
         }
     }
     p.infos = (SharedInfo*)((char*)ws_or_null + off);
-    off += (size_t)2 * d.B * sizeof(SharedInfo);
+    off += ((size_t)2 * d.B * sizeof(SharedInfo) + 255) / 256 * 256;
     p.ws_bytes = off;
     return p;
 }
