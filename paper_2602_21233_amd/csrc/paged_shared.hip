@@ -12,19 +12,20 @@ constexpr int kCutThreads = 1024;
 constexpr int64_t kMostUnits = 1 << 30;
 
 // sum or maximum over the workgroup, in every thread
-template <int N, typename T, typename F>
-__device__ __forceinline__ void over_workgroup(T (&v)[N], T (*s)[kCutThreads / 64], F&& join) {
+template <int N, typename F>
+__device__ __forceinline__ void over_workgroup(float (&v)[N], float (*s)[kCutThreads / 64], F&& join) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int x = 0; x < N; ++x) {
+    for (int y = 1; y < 64; y <<= 1)
 #pragma unroll
-        for (int y = 1; y < 64; y <<= 1) v[x] = join(v[x], (T)__shfl_xor(v[x], y));
+        for (int x = 0; x < N; ++x) v[x] = join(x, v[x], __shfl_xor(v[x], y));
+#pragma unroll
+    for (int x = 0; x < N; ++x)
         if (lane == 0) s[x][wave] = v[x];
-    }
     __syncthreads();
     for (int w = 0; w < (int)blockDim.x / 64; ++w)
 #pragma unroll
-        for (int x = 0; x < N; ++x) v[x] = w == 0 ? s[x][0] : join(v[x], s[x][w]);
+        for (int x = 0; x < N; ++x) v[x] = w == 0 ? s[x][0] : join(x, v[x], s[x][w]);
     __syncthreads();
 }
 
@@ -33,63 +34,60 @@ __device__ __forceinline__ void over_workgroup(T (&v)[N], T (*s)[kCutThreads / 6
 // of a few loads and sums that wait for each other.
 template <int EACH>
 __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, PagedPart few, PagedPart many) {
-    __shared__ long long s_sum[8][kCutThreads / 64];
+    __shared__ float s_sum[8][kCutThreads / 64];
     __shared__ int s_scan[2][2][kCutThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = 2 * a.B, threads = blockDim.x;
-    SharedInfo info[EACH];                         // of share threads * i + tid
+    SharedInfo info;                               // of the last share looked at; shares threads * i + tid are this thread's
     int tiles[EACH], keys[EACH];                   // tiles of the kernel for many rows negative
-    auto add = [](long long x, long long y) { return x + y; };
-    auto top = [](long long x, long long y) { return x > y ? x : y; };
-    long long sums[3] = {0, 0, 0};                 // (row tile, key tile) pairs of few and many rows, row tiles of many
+    // Work is summed in fp32: it decides how long pieces are, and with a little more than the sum they never take more than the workspace's room.
+    float sums[3] = {0.f, 0.f, 0.f};               // (row tile, key tile, KV head) triples of few and many rows, row tiles of many
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        info[i] = shared_range(a, threads * i + tid);          // empty behind the last share
-        const PagedShare f = few.m ? shared_share(few, a.G, info[i], a.sink, a.window) : PagedShare{0, 0, 1};
-        const PagedShare m = shared_share(many, a.G, info[i], a.sink, a.window);
+        info = shared_range(a, threads * i + tid);             // empty behind the last share
+        const PagedShare f = few.m ? shared_share(few, a.G, info, a.sink, a.window) : PagedShare{0, 0, 1};
+        const PagedShare m = shared_share(many, a.G, info, a.sink, a.window);
         tiles[i] = f.tiles > 0 ? f.tiles : -m.tiles;
         keys[i] = f.tiles > 0 ? f.keys : m.keys;
-        sums[0] += (long long)f.tiles * f.keys;
-        sums[1] += (long long)m.tiles * m.keys;
-        sums[2] += m.tiles;
+        sums[0] += (float)f.tiles * (float)f.keys * (float)a.Hkv;
+        sums[1] += (float)m.tiles * (float)m.keys * (float)a.Hkv;
+        sums[2] += (float)m.tiles * (float)a.Hkv;
     }
-    over_workgroup(sums, s_sum, add);
-    const long long work = sums[1] * a.Hkv, row_tiles = sums[2] * a.Hkv;
-    const int few_piece = few.m ? few_rows_piece(sums[0] * a.Hkv, few) : kWholeAxis;
+    over_workgroup(sums, s_sum, [](int, float x, float y) { return x + y; });
+    auto rounded_up = [](float x) { return (int64_t)(x * 1.0001f) + 1; };
+    const int few_piece = few.m ? few_rows_piece(rounded_up(sums[0]), few) : kWholeAxis;
 
-    // many rows: the least time of four lengths
-    const int least = shortest_piece(work, many);
-    auto pieces_of = [&](long long n) { return n > row_tiles ? piece_within((long long)ceilf((float)work / (float)(n - row_tiles)), many) : kWholeAxis; };
-        // 512 workgroups run at once.  Those of few rows go beside the others, which get their share of the places by time: a key tile of few rows is
-    // bound by the memory and counts for one and a half of many rows', but 200 of them have all that the memory gives (16 requests
-    // of 7 prompts of 23000, as much of either: 212 us with 178 places for many rows, 157 with 280, 176 with 512).  64 requests of 4 prompts, 8000 key tiles of many rows and 6144 of few, with 256, 384,
-    // 512 and 1024 pieces of many rows: 110.8, 115.5, 119.5 and 131.6 us; 8 behind 100000, 12500 and 448: 119.5, 113.6, 102.7 and 120.0.
-    const float share = sums[1] > 0 ? (float)sums[1] / ((float)sums[1] + 1.5f * (float)sums[0]) : 1.f;
-    const int places = max(280, (int)(512.f * share));
-    const int fit = pieces_of(places);
-    int p[4] = {kWholeAxis, fit, fit < kWholeAxis / 4 ? 2 * fit : kWholeAxis, fit < kWholeAxis / 4 ? 4 * fit : kWholeAxis};
-    long long units[4] = {0, 0, 0, 0}, longest[4] = {0, 0, 0, 0};
+    // Many rows: the least time of four lengths.  512 workgroups run at once.  Those of few rows go beside the others, which get their share of the
+    // places by time: a key tile of few rows is bound by the memory and counts for one and a half of many rows', but 200 of them have all
+    // that the memory gives (16 requests of 7 prompts of 23000, as much of either: 212 us with 178 places for many rows, 157 with 280, 176 with 512).  64
+    // requests of 4 prompts, 8000 key tiles of many rows and 6144 of few, with 256, 384, 512 and 1024 pieces of many rows: 110.8, 115.5, 119.5 and
+    // 131.6 us; 8 behind 100000, 12500 and 448: 119.5, 113.6, 102.7 and 120.0.
+    int many_piece = kWholeAxis;
+    if (sums[2] > 0.f) {
+        const float places = fmaxf(280.f, 512.f * sums[1] / fmaxf(sums[1] + 1.5f * sums[0], 1.f));
+        const int least = shortest_piece(rounded_up(sums[1]), many);
+        const int fit = places > sums[2] ? piece_within((int64_t)ceilf(sums[1] / (places - sums[2])), many) : kWholeAxis;
+        int p[4] = {kWholeAxis, fit, fit < kWholeAxis / 4 ? 2 * fit : kWholeAxis, fit < kWholeAxis / 4 ? 4 * fit : kWholeAxis};
+        float v[8];                                // units, longest piece
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        p[t] = p[t] < least ? least : (p[t] > kWholeAxis ? kWholeAxis : p[t]);
+        for (int t = 0; t < 4; ++t) {
+            p[t] = p[t] < least ? least : p[t];
+            v[t] = v[4 + t] = 0.f;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            if (tiles[i] >= 0) continue;
-            const int splits = pieces_for(keys[i], p[t]);
-            units[t] += (long long)-tiles[i] * splits * a.Hkv;
-            longest[t] = top(longest[t], keys[i] < p[t] ? keys[i] : p[t]);
+            for (int i = 0; i < EACH; ++i) {
+                if (tiles[i] >= 0) continue;
+                v[t] += (float)-tiles[i] * (float)pieces_for(keys[i], p[t]) * (float)a.Hkv;
+                v[4 + t] = fmaxf(v[4 + t], (float)min(keys[i], p[t]));
+            }
         }
-    }
-    over_workgroup(units, s_sum, add);
-    over_workgroup(longest, s_sum, top);
-    int many_piece = p[0];
-    float best = INFINITY;
+        over_workgroup(v, s_sum, [](int x, float y, float z) { return x < 4 ? y + z : fmaxf(y, z); });
+        float best = INFINITY;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const float n = (float)(units[t] > 1 ? units[t] : 1);
-        const float us = 1.6f * fmaxf((float)longest[t], ceilf(n / (float)places) * (float)work / n) + 0.03f * n;
-        if (us < best) {
-            best = us;
-            many_piece = p[t];
+        for (int t = 0; t < 4; ++t) {
+            const float n = fmaxf(v[t], 1.f), us = 1.6f * fmaxf(v[4 + t], ceilf(n / places) * sums[1] / n) + 0.03f * n;
+            if (us < best) {
+                best = us;
+                many_piece = p[t];
+            }
         }
     }
     int base[2] = {0, 0};
@@ -122,9 +120,10 @@ __global__ __launch_bounds__(kCutThreads) void paged_cut_kernel(PagedArgs a, Pag
         }
         if (e < E) {
             const bool is_few = tiles[i] > 0;
-            info[i].before = (is_few ? end[0] : end[1]) - (is_few ? own[0] : own[1]);
-            info[i].splits = tiles[i] == 0 ? 0 : pieces_for(keys[i], is_few ? few_piece : many_piece);
-            a.infos[e] = info[i];
+            if (EACH > 1) info = shared_range(a, e);
+            info.before = (is_few ? end[0] : end[1]) - (is_few ? own[0] : own[1]);
+            info.splits = tiles[i] == 0 ? 0 : pieces_for(keys[i], is_few ? few_piece : many_piece);
+            a.infos[e] = info;
         }
     }
 }
