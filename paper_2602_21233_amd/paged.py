@@ -100,17 +100,18 @@ def _cache(k_pages, vt_pages, dtype=_BF16):
 
 def _exps(k_exp, v_exp, device, n, h, p):
     """The packed SpaPagedExps of the exponents of a cache."""
-    at = []
-    for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
-        if t is None or t.dtype is not torch.uint8 or t.device != device or t.shape != (n, h, p):
-            raise TypeError(f"{name} must be a uint8 tensor [{n}, {h}, {p}] on {device}")
-        page, head, inner = t.stride()
-        if inner != 1:
-            raise TypeError(f"the last axis of {name} must be contiguous")
-        if h == 1:
-            head = p
-        at += [page if n > 1 else h * head, head]
-    return _EXPS.pack(k_exp.data_ptr(), v_exp.data_ptr(), *at)
+    if k_exp is None or v_exp is None or k_exp.dtype is not torch.uint8 or v_exp.dtype is not torch.uint8 or k_exp.device != device \
+            or v_exp.device != device or k_exp.shape != (n, h, p) or v_exp.shape != (n, h, p):
+        raise TypeError(f"k_exp and v_exp must be uint8 tensors [{n}, {h}, {p}] on {device}")
+    k0, k1, k2 = k_exp.stride()
+    v0, v1, v2 = v_exp.stride()
+    if k2 != 1 or v2 != 1:
+        raise TypeError("the last axes of k_exp and v_exp must be contiguous")
+    if h == 1:
+        k1 = v1 = p
+    if n == 1:
+        k0, v0 = h * k1, h * v1
+    return _EXPS.pack(k_exp.data_ptr(), v_exp.data_ptr(), k0, k1, v0, v1)
 
 
 def _launch(name, device, *args):
