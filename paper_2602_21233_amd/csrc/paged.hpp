@@ -129,8 +129,10 @@ __host__ __device__ __forceinline__ PagedShare shared_share(const PagedPart& par
         const bool common = r.members > 0;
         const int all = (common ? r.end : (r.kv + kPagedTile - 1) / kPagedTile) - r.tile;
         s.tiles = (int)((rows + part.m - 1) >> part.log_m);
-        // the rows of a group are those of several requests, with windows of their own
-        s.keys = common ? all : most_key_tiles(r.len, r.kv, part.span, sink, window);
+        // Rows of a group are behind what it has in common, so their windows reach that far back into it at most; one that is not may have more
+        // tiles, which the last piece takes.
+        const int64_t reach = (int64_t)(sink + kPagedTile - 1) / kPagedTile + ((int64_t)window + kPagedTile - 2) / kPagedTile;
+        s.keys = !common ? most_key_tiles(r.len, r.kv, part.span, sink, window) : window > 0 && reach < all ? (int)reach : all;
         if (s.keys > all) s.keys = all;
         if (s.keys < 0) s.keys = 0;
     }

@@ -420,7 +420,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
         else return key_tiles(pos_lo, pos_hi, a.sink, a.window);
     }();
     const int per = tiles_of_piece(sh.s);
-    const int e_end = min((cut + 1) * per, kt.n);               // of the row tile's key tiles
+    const int e_end = SHARED && cut == sh.s.splits - 1 ? kt.n : min((cut + 1) * per, kt.n);     // of the row tile's key tiles
     const bool to_last = e_end == kt.n && (!SHARED || kt.n == 0 || kt.at(kt.n - 1) == pos_hi / kPagedTile);      // the tile of pos_hi is the last one
     const int last_key = !SHARED || unit.range.end > pos_hi / kPagedTile ? pos_hi : unit.range.end * kPagedTile - 1;
     const int last_col = last_key >= 0 ? last_key >> a.log_p : 0;
@@ -982,7 +982,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
     }();
     const int per = tiles_of_piece(sh.s);
     const int e0 = cut * per;
-    const int n_st = min((cut + 1) * per, kt.n) - e0;                         // key tiles of this workgroup
+    const int n_st = (SHARED && cut == sh.s.splits - 1 ? kt.n : min((cut + 1) * per, kt.n)) - e0;     // key tiles of this workgroup
     bool partial = sh.s.splits > 1;
     if constexpr (SHARED) partial = unit.partial;
     const int slot = sh.slot + sh.unit;

@@ -108,6 +108,19 @@ def test_values_that_are_not_finite_under_a_shared_prompt(spa, requests, window,
             assert torch.equal(got[step.starts[b] + i].nan_to_num(7e9), want.nan_to_num(7e9)), (b, i)
 
 
+@pytest.mark.parametrize("q8", [False, True], ids=["bf16", "q8"])
+@pytest.mark.parametrize("sink,window", [(0, 100), (70, 300), (5, 1)])
+def test_a_request_left_out_does_not_cut_the_others_window(spa, sink, window, q8):
+    """Rows of requests without keys, or with fewer than the group has in common, lie in one tile with others."""
+    step = oracle.Step(3, [(640, [(5, 1), (0, 2), (9, 1), (70, 30)])], q_heads=4, kv_heads=2, head_dim=64, q8=q8)
+    for b, kv in ((2, 0), (1, 200), (0, 3)):
+        step.kv_lens[b] = kv
+        how = dict(sink=sink, window=window)
+        want, _, tol, _ = step.want(**how)
+        got = _attn(spa, step, shares=step.shares, n_sink_tokens=sink, window_tokens=window)
+        assert ((got.cpu().double() - want).abs() - tol).max().item() <= 0
+
+
 # ----------------------------------------------------------------------------------------------------- malformed inputs
 def _guarded(shape, dtype, fill):
     """A tensor in the middle of an allocation whose rest must not change."""
