@@ -184,7 +184,7 @@ __device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedPart& p
 }
 // ---------------------------------------------------------------------------------------------------------------
 // Shared prompts.  The rows of a group are the new tokens of its requests, which follow each other; they attend to the key tiles that the group has
-// in common, and each request's to its other ones.  A kernel of one workgroup (paged_attn_shared.hip) has cut the call: part.unit_end.  Every part
+// in common, and each request's to its other ones.  A kernel of one workgroup (paged_shared.hip) has cut the call: part.unit_end.  Every part
 // of a query that has more than one leaves a partial result, in the place of its workgroup.
 
 // whole key tiles in pages that the group of request b has in common, 0 where it has none; leader: its first request, n: how many there are
@@ -1384,6 +1384,9 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         constexpr int PAR = decltype(par_tag)::value;      // t % 2
         using KB = IC<1 - PAR>;
         using VB = IC<PAR>;
+        // Of two wavefronts of a SIMD the one in its products goes first, and the other waits, converts and asks for its next tile meanwhile (chunk of
+        // 2048 tokens 2990 -> 2937 us, mixed step 381 -> 373; quantised 3550 -> 3350, where the loads' addresses go first, too: 3384 else).
+        __builtin_amdgcn_s_setprio(0);
         if (t > 0) {                                       // K(t + 1) and V^T(t) have been requested
             if constexpr (Q8) {                            // the buffers were last read before the barrier of tile t - 1
                 Places at;
@@ -1397,6 +1400,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
             }
         }
         __syncthreads();                                   // they are there, and the buffers refilled below have been read
+        if constexpr (Q8) __builtin_amdgcn_s_setprio(2);
         bf16x8 f[4];
         f[0] = lds16(ldsK + KB::value * TILE_B + kofs[0]);
         f[1] = lds16(ldsV + VB::value * TILE_B + vofs[0]);
@@ -1411,6 +1415,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         pg1 = pg2;
         pg2 = pages_of(t + 3);
         if (t + 1 < first_tile) return;
+        __builtin_amdgcn_s_setprio(2);
         step(KB{}, VB{}, IC<0>{}, key_of(t) + 32, sB, sA, pA0, pA1, pB0, pB1, f);
         // past the end: products of a stale buffer, masked like keys behind every position
         step(KB{}, VB{}, IC<1>{}, t + 1 < n_st ? key_of(t + 1) : 1 << 30, sA, sB, pB0, pB1, pA0, pA1, f);
@@ -1421,6 +1426,8 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedPart& p
         one_tile(IC<1>{}, t);
         if (++t == n_st) break;
     }
+
+    __builtin_amdgcn_s_setprio(0);
 
     // Infinite and NaN values that were taken out, for the rows that see them: rare, so it looks through all the tiles again
     __syncthreads();
