@@ -341,6 +341,11 @@ __device__ __forceinline__ bf16x8 bf16_of(uint32_t lo, uint32_t hi, float scale)
 __device__ __forceinline__ float max_over_groups(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
 __device__ __forceinline__ float sum_over_groups(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
 
+// The pages of a wavefront's keys, by scalar loads: a vector load behind a tile's own ones would be waited for together with all of them, and its
+// value is needed before the next tile's can be asked for (many rows: mixed step 397 -> 385 us; few rows, 64 quantised requests 115.4 -> 114.1).
+typedef __attribute__((address_space(4))) const int32_t scalar_i32;
+__device__ __forceinline__ scalar_i32* scalar_pointer(const int32_t* p) { return (scalar_i32*)(uintptr_t)p; }
+
 // ---------------------------------------------------------------------------------------------------------------
 // Few rows: MF * 16 rows, NW wavefronts that each take every NW-th 32 keys, straight from memory into the operands of
 // v_mfma_f32_16x16x32_bf16 (S^T = K Q^T, O^T += V^T P^T).  A lane holds keys 8 (lane / 16) .. + 7 of a chunk of one row:
@@ -453,6 +458,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
     // chunks of this workgroup: the last tile's second half only if a row sees it
     const int c_end = CPT == 2 && to_last && (pos_hi & (kPagedTile - 1)) < 32 ? 2 * e_end - 1 : CPT * e_end;
     auto key_of = [&](int c) { return CPT == 2 ? kt.at(c >> 1) * kPagedTile + 32 * (c & 1) : kt.at(c) * kPagedTile; };
+    auto entry_of = [&](int key) { return scalar_pointer(trow)[min(key >> a.log_p, last_col)]; };     // key: the same in every lane
     struct Pages {                                              // small pages: a chunk lies in NP of them
         int id[NP == 1 ? 1 : 2];                                // Q8: those that this lane's K rows and its values are in, else both
     };
@@ -460,7 +466,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
         Pages p;
         const int key0 = key_of(min(c, c_end - 1));
         if constexpr (NP == 1) {
-            p.id[0] = page_of(key0);
+            p.id[0] = entry_of(key0);                           // clamped where it is used, so that nothing waits for it here
         } else if constexpr (Q8) {
             p.id[0] = page_of(key0 + NX * (n16 >> 2));
             p.id[1] = page_of(key0 + NX * g);
@@ -473,7 +479,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedPart& pa
     };
     // the page of keys NX quarter .. + NX - 1 of a chunk, a lane's K rows or its values, and the first one's place in it
     auto id_of = [&](const Pages& pg, int quarter, bool values) {
-        if constexpr (NP == 1) return pg.id[0];
+        if constexpr (NP == 1) return clamp_int(pg.id[0], 0, a.n_pages - 1);
         else if constexpr (Q8) return values ? pg.id[1] : pg.id[0];
         else return quarter >= 2 ? pg.id[1] : pg.id[0];
     };
@@ -898,11 +904,6 @@ __device__ __forceinline__ void group_mode_weights(const f32x16& s, const ChunkW
         else { exps(4, 4); finish(); }
     }
 }
-
-// The pages of a wavefront's keys, by scalar loads: a vector load behind a tile's own ones would be waited for together with all of them, and its
-// value is needed before the next tile's can be asked for (time of a tile of quantised keys 2.36 -> 2.0 us).
-typedef __attribute__((address_space(4))) const int32_t scalar_i32;
-__device__ __forceinline__ scalar_i32* scalar_pointer(const int32_t* p) { return (scalar_i32*)(uintptr_t)p; }
 
 // 16 bytes per lane straight into LDS, each lane from an address of its own
 template <int IMM>
