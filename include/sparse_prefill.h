@@ -491,7 +491,8 @@ typedef struct spa_paged_exps {
  * key and value apart, the exponent e that is the least with max |x_d| <= 448 * 2^e over the finite x_d (at least -126, and -126
  * where all are 0); the page gets x_d 2^-e rounded to the nearest e4m3 value, ties to even, and the exponent's place e + 127.  A power of two
  * makes both the quotient and the value that is read back exact, and e4m3 keeps its precision down to 2^-14 of the row's maximum.
- * Infinities and NaN become NaN.  Values are meant to be below 2^119: larger ones may stand for more than bf16 holds.
+ * Infinities and NaN become NaN.  Values are meant to be below 2^119: larger ones may stand for more than bf16 holds.  A slot must occur
+ * only once: where it occurs more often its place may hold one token's values with another one's exponent, or some of either.
  * Uses of p: n_kv_heads, head_dim, page_size, n_pages, n_tokens, strides. */
 int sparse_prefill_paged_append_quantised(const spa_paged_params *p, const void *k, const void *v, const int32_t *slots,
                                    void *k_pages, void *vt_pages, const spa_paged_exps *exps, void *hip_stream);
@@ -536,7 +537,10 @@ int spa_paged_shared_workspace_bytes(const spa_paged_params *p, size_t *bytes);
 /* sparse_prefill_paged_attn (exps_or_null NULL) or sparse_prefill_paged_attn_quantised for requests that share prompts: the same sums, but the queries of
  * a group attend together to what they have in common, which is read once for all of them through the table row of the group's first request,
  * and each request to the rest by itself; the parts are joined by their log-sum-exps.  shares: as above, read on the device; where the rows of
- * a group do not have shares[2] tokens in common pages its results are unspecified. */
+ * a group do not have shares[2] tokens in common pages its results are unspecified.  max_new_tokens is not looked at.
+ * What has more than 16 rows (new tokens of the group or of a request * query heads of a KV head; 32 where these heads are 17 to 32) goes
+ * through the kernel for many rows.  ws: spa_paged_shared_workspace_bytes() bytes (two fp32 results of every row, and more for cuts), 256-byte
+ * aligned; its contents need not survive between calls, calls that overlap in time need one each. */
 int sparse_prefill_paged_attn_shared(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,
                                      const spa_paged_exps *exps_or_null, const int32_t *block_table,
                                      const int32_t *q_starts, const int32_t *kv_lens, const int32_t *shares,

@@ -353,6 +353,11 @@ __device__ __forceinline__ scalar_i32* scalar_pointer(const int32_t* p) { return
 // by HBM: nothing is shared between the wavefronts, so there is no LDS in the loop and no barrier.
 // 64 requests of up to 8192 keys: 205 to 207 us for 1.14 GB of keys and values, 5.5 TB/s (a plain sum of 2 GiB: 6.07).
 //
+// Q8: chunks of 64 keys, 16 dims of a key or 16 keys of a dim in a lane's 16 bytes; which of an operand's rows a dim or key is is free, as long
+// as the other operand agrees.  A key's power of two goes into its conversion (exact in bf16), a value's to its weight: the keys of a lane's
+// values differ.  The same requests: 107 to 110 us for 0.575 GB, 5.3 TB/s.  Two wavefronts of a SIMD instead of three where 168 registers do not hold
+// them (small pages, caps and slopes with head_dim 128).
+//
 // NV > 1: a workgroup makes the outputs of D / NV dims only, from all of K and its share of V.  A CU takes in about 12 bytes a
 // clock however many loads it has in flight (256 KB of a head: 22000 cycles of a call of 501 keys), so a call of few workgroups
 // is faster on NV times as many, although they read K NV times: 11.8 -> 9.2 us.  The host tells few workgroups from the table's width: the same
@@ -815,7 +820,7 @@ __global__ __launch_bounds__(64 * NW, MF > 1 || (Q8 && D == 128 && (NP > 1 || MO
 // four share through LDS: the pipeline step of the sparse prefill's attention kernel (attn.hip: direct loads into a double
 // buffer, logits two 32-key chunks ahead of the second product, one barrier a tile), with pages in place of blocks, masks
 // where a tile needs them instead of in the last block, and logits that may be capped or biased.  2048 tokens over 98304 of 32 / 8
-// heads: 2.97 to 3.2 ms by card, 1.03 to 1.12 PFLOP/s (a plain product of 8192^3: 1.33), matrix cores busy 56 % at 1.8 GHz; with
+// heads: 2.94 to 3.1 ms by card, 1.06 to 1.13 PFLOP/s (a plain product of 8192^3: 1.33), matrix cores busy 56 % at 1.8 GHz; with
 // head_dim 64, where the exponentials weigh twice as much, 0.78 to 0.84, capped 0.88 to 0.91 and 0.56.
 // The keys are taken from the last tile to the first: with a bias that falls with the distance a row then meets its largest
 // logits first and its reference hardly moves.
@@ -1646,7 +1651,7 @@ void launch_many(const PagedArgs& a, const PagedParts& parts, int64_t many_grid,
 template <int D, bool Q8>
 hipError_t launch_parts(const PagedArgs& a, const PagedDims& d, const PagedParts& parts, hipStream_t st) {
     // A call with requests of both kinds runs them side by side, the many-row workgroups first: the ones wait for the matrix cores, the
-    // others for the memory (mixed step 431 -> 399 us, 10 short prompts and single tokens 24.8 -> 19.3).  With 17 to 32 query heads of a KV head, one after the other.
+    // others for the memory (mixed step 431 -> 399 us, now 373; 10 short prompts and single tokens 24.8 -> 19.3).  With 17 to 32 query heads of a KV head, one after the other.
     const bool both = parts.many.m && parts.few.m == 16;
     const int64_t few_grid = parts.few.m ? most_units(d, parts.few) : 0, many_grid = parts.many.m ? most_units(d, parts.many) : 0;
     if (few_grid + many_grid > 0x7fffffffll) return hipErrorInvalidValue;

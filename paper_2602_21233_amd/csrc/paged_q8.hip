@@ -36,7 +36,8 @@ __device__ __forceinline__ uint2 quantise8(const float (&x)[8], uint32_t e) {
     return make_uint2(to_e4m3(y[0], y[1], y[2], y[3]), to_e4m3(y[4], y[5], y[6], y[7]));
 }
 
-// A thread quantises 8 dims of a token's key and value; D / 8 lanes share their row's maximum.
+// Few tokens: a thread quantises 8 dims of a token's key and value; D / 8 lanes share their row's maximum.  Bound by latency and the single-byte stores of V
+// (256 scattered tokens of 8 heads of 128: 6.8 us).
 template <int D>
 __global__ __launch_bounds__(256) void paged_append_q8_kernel(const uint16_t* __restrict__ k, int64_t k_t, int64_t k_h, const uint16_t* __restrict__ v,
                                                               int64_t v_t, int64_t v_h, const int32_t* __restrict__ slots, uint8_t* __restrict__ k_pages,
@@ -73,7 +74,8 @@ struct ReadArgs {
     int B, Hkv, T, C, log_p, n_pages;
 };
 // A wavefront reads 64 positions (a tile) x 64 dims of a head, a lane 8 positions x 8 dims: K rows as they are, V^T pieces of 8 positions transposed
-// in registers, both to whole 128-byte lines.  The tiles of the requests follow each other; every wavefront finds its own.
+// in registers, both to whole 128-byte lines.  The tiles of the requests follow each other; every wavefront finds its own.  Bound by HBM: 98304 quantised
+// tokens 121 us, 605 MB at 5.0 TB/s; 28000 tokens of bf16 pages of 16, head_dim 64, 30 us, 4.9 TB/s (a plain copy of 2 GiB: 4.9).
 template <bool Q8>
 __global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a, int dim_parts) {
     const int lane = threadIdx.x & 63;
@@ -175,7 +177,8 @@ __global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a, int dim_par
 
 // Many tokens: a wavefront moves 32 tokens x 128 dims (with head_dim 64, of two heads), a lane 8 tokens (a window) x 8 dims.  Where 8 tokens that follow
 // each other fill an aligned 8-byte piece of a page's V rows (those of a prompt do, wherever its chunk starts), the lanes that have the first of
-// them in their window load all 8, quantise and transpose them in registers and store the pieces whole; the others are stored value by value.
+// them in their window load all 8, quantise and transpose them in registers and store the pieces whole; the others are stored value by value.  Bound by HBM: 16384 tokens of 8
+// prompts, 121 MB, 30 us, 4.0 TB/s (value by value: 183 us).
 template <int D>
 __global__ __launch_bounds__(256) void paged_append_q8_runs_kernel(const uint16_t* __restrict__ k, int64_t k_t, int64_t k_h, const uint16_t* __restrict__ v,
                                                                    int64_t v_t, int64_t v_h, const int32_t* __restrict__ slots,
@@ -275,7 +278,8 @@ __global__ __launch_bounds__(256) void paged_append_q8_runs_kernel(const uint16_
     }
 }
 
-// Tokens up to which paged_append_q8_kernel moves them, the other kernel more.
+// Tokens up to which paged_append_q8_kernel moves them, the other kernel more: 1024 single tokens 15.0 us with the one, 1025 21.1 with the other, of a prompt
+// 8.6 and 8.5.
 constexpr int kFewAppended = 1024;
 template <int D>
 hipError_t launch_append(const PagedDims& d, const void* k, int64_t k_t, int64_t k_h, const void* v, int64_t v_t, int64_t v_h,
