@@ -499,7 +499,8 @@ int sparse_prefill_paged_append_quantised(const spa_paged_params *p, const void 
 
 /* sparse_prefill_paged_attn over a quantised cache: the same sums over the values that pages and exponents stand for, which enter the
  * matrix products exactly; same options, precision, workspace (spa_paged_workspace_bytes) and treatment of what is not finite or not seen.
- * What lies behind a request's last key may be anything here, too, exponents among it. */
+ * What lies behind a request's last key may be anything here, too, exponents among it.  A value's power of two enters the kernel for few rows with its
+ * weight, in 32 and twice 8 bits: values are meant to be rows with a maximum of 2^-86 or more, or zero; smaller ones lose precision there. */
 int sparse_prefill_paged_attn_quantised(const spa_paged_params *p, const void *q, const void *k_pages, const void *vt_pages,
                                  const spa_paged_exps *exps, const int32_t *block_table, const int32_t *q_starts,
                                  const int32_t *kv_lens, const float *slopes_or_null, void *out, float *lse_or_null,
