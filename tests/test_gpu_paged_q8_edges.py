@@ -367,6 +367,55 @@ def test_more_requests_than_a_workgroup_has_threads(spa):
     assert torch.equal(found.cpu(), oracle.shares(step.table, step.starts, step.kv_lens, 16, 16))
 
 
+@pytest.mark.parametrize("q8", [False, True], ids=["bf16", "q8"])
+def test_shared_attention_of_strided_tensors_and_one_workspace_for_many_calls(spa, q8):
+    step = oracle.Step(3, [(300, [(20, 1), (0, 9)]), (70, [(5, 40), (1, 1), (0, 1)])], q_heads=6, kv_heads=2, page=64, q8=q8)
+    T, B, N, C = step.T, 5, step.k_pages.shape[0], step.table.shape[1]
+    kp, vp, ke, ve = step.cache()
+    lens = _i32(step.starts), _i32(step.kv_lens)
+    plain, lse = spa.paged_attn_shared(step.q.cuda(), kp, vp, step.table.cuda(), *lens, step.shares.cuda(), ke, ve, return_lse=True)
+    qkv = torch.full((T, 10, 144), math.nan, dtype=torch.bfloat16, device="cuda")
+    qkv[:, 2:8, 8:136] = step.q.cuda()
+    both = torch.stack([kp.flatten(2).view(torch.uint8 if q8 else torch.bfloat16), vp.flatten(2).view(torch.uint8 if q8 else torch.bfloat16)], 1)
+    k, v = both[:, 0].view(N, 2, 64, 128), both[:, 1].view(N, 2, 128, 64)
+    if q8:
+        k, v = k.view(E4M3), v.view(E4M3)
+        both_exps = torch.stack([ke, ve], 2)
+        ke, ve = both_exps[:, :, 0], both_exps[:, :, 1]
+    wide = torch.full((B, 50), -1, dtype=torch.int32, device="cuda")
+    wide[:, 3:3 + C] = step.table.cuda()
+    room = torch.full((6, T, 160), 7.0, dtype=torch.bfloat16, device="cuda")
+    need = spa.paged_shared_workspace_bytes(spa.make_paged_params(batch=B, n_q_heads=6, n_kv_heads=2, head_dim=128, page_size=64, n_pages=N, max_pages=C, n_tokens=T,
+                                                                  table_stride=50))
+    workspace = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    for turn in range(3):
+        got, again = spa.paged_attn_shared(qkv[:, 2:8, 8:136], k, v, wide[:, 3:3 + C], *lens, step.shares.cuda(), ke, ve, out=room[:, :, 16:144].transpose(0, 1),
+                                           workspace=workspace, return_lse=True)
+        assert torch.equal(got.view(torch.int16), plain.view(torch.int16)) and torch.equal(again, lse), turn
+        assert (room[:, :, :16] == 7.0).all() and (room[:, :, 144:] == 7.0).all()
+        room.fill_(7.0)
+        spa.paged_attn_shared(step.q.cuda()[:14], kp, vp, step.table.cuda()[:2], _i32([0, 1, 10]), lens[1][:2], step.shares[:, :2].cuda().contiguous(),
+                              *step.cache()[2:], workspace=workspace)
+    rows_k, rows_v = spa.paged_read(k, v, wide[:, 3:3 + C], _i32([0, 3, 3, 40, 41, 41]), lens[1], 41, ke, ve)
+    assert torch.equal(rows_k[3:40].cpu(), step.keys[2][:, -37:].transpose(0, 1)) and torch.equal(rows_v[:3].cpu(), step.values[0][:, -3:].transpose(0, 1))
+
+
+@pytest.mark.parametrize("n", [1, 31, 1024, 1025])
+def test_append_of_either_kernel_leaves_the_same_bytes(spa, n):
+    """A prompt that starts inside a page, in one call and token by token (33 at a time)."""
+    page, H, D = 32, 3, 64
+    x = torch.randn(2, n, H, D, generator=torch.Generator().manual_seed(n)).to(torch.bfloat16).cuda()
+    slots = torch.arange(5, 5 + n, dtype=torch.int32, device="cuda")
+    caches = []
+    for size in (n, 33):
+        c = [torch.full(s, 9, dtype=torch.uint8, device="cuda") for s in ((40, H, page, D), (40, H, D, page), (40, H, page), (40, H, page))]
+        for at in range(0, n, size):
+            part = slice(at, at + size)
+            spa.paged_append_q8(x[0, part], x[1, part], slots[part].contiguous(), c[0].view(E4M3), c[1].view(E4M3), *c[2:])
+        caches.append(c)
+    assert all(torch.equal(a, b) for a, b in zip(*caches))
+
+
 def test_nothing_to_do(spa):
     """No tokens at all, one request, the shortest lengths."""
     step = oracle.Step(1, [(64, [(0, 1), (0, 1)])], q8=True, padding=5)
